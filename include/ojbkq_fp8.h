@@ -1,0 +1,91 @@
+/*
+ * ojbkq_fp8.h -- C ABI of the 8-bit floating point side of the library: the
+ * activations of a linear layer in 8 bits, and the layer's product with them.
+ *
+ * A layer quantized by the calls of ojbkq.h is applied as W_hat = S (Q - Z)
+ * (the Q, S, Z data model of Sec. 3.2) to activations in 16 bits
+ * (ojbkq_dequant_matmul).  The calls here bring the activations to 8 bits --
+ * by themselves, or as the output of the norm in front of the layer -- and
+ * multiply them with such a layer, or with weights that are 8-bit floating
+ * point numbers themselves.
+ *
+ * Number formats (those of the OCP 8-bit and microscaling specifications)
+ *   e4m3  sign, 4 exponent bits, 3 mantissa bits; largest 448, smallest
+ *         2^-9; no infinity, one NaN (0x7f, 0xff).
+ *   e8m0  a power of two 2^(code - 127) in a byte (code 255, NaN, is never
+ *         written).
+ *   A scale that is a power of two costs a floating point format nothing
+ *   (multiplying by it is exact).
+ *
+ * An 8-bit array is [rows, m] e4m3 values, features contiguous, row stride ld
+ * (bytes), with one e8m0 scale for each block of `block_rows` rows (1 or 128)
+ * x 128 features: [ceil(rows / block_rows), G], G = ceil(m / 128), row stride
+ * lds (bytes).  It stands for value x scale.  The values are 16-byte aligned,
+ * ld is a multiple of 16 and at least m rounded up to 16; the scales are 4-byte
+ * aligned, lds is a multiple of 4 and at least G rounded up to 4.  Every row
+ * (the last one too) is readable up to these roundings; what stands there is
+ * not used.
+ *
+ * Conventions otherwise as in ojbkq.h: device pointers owned by the caller, no
+ * device memory allocated, argument errors (OJBKQ_EINVAL) before anything is
+ * enqueued, messages through ojbkq_last_error().  Every call is asynchronous
+ * on `stream`, which must belong to the current device, and can be captured
+ * into a HIP graph.  Results depend only on the inputs.
+ */
+#ifndef OJBKQ_FP8_H
+#define OJBKQ_FP8_H
+
+#include "ojbkq.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Features to a scale. */
+#define OJBKQ_FP8_BLOCK 128
+
+/* Types of the arrays that are not in 8 bits. */
+enum { OJBKQ_F32 = 0, OJBKQ_F16 = 1, OJBKQ_BF16 = 2 };
+
+/* Types of the scales of 8-bit weights. */
+enum { OJBKQ_SCALE_F32 = 0, OJBKQ_SCALE_E8M0 = 1 };
+
+/* X brought to 8 bits.  With a the largest finite magnitude of a block, its
+ * scale is 2^e with the least e >= -127 for which a <= 448 2^e (2^0 where a =
+ * 0), and its values are e4m3(x 2^-e), to nearest even.  Infinities and NaN
+ * become NaN and leave the others alone.
+ *   X: type xtype (OJBKQ_F32, _F16, _BF16).  features_first = 0: [rows, m],
+ *   row stride ldx >= m (elements).  features_first = 1: [m, rows], row stride
+ *   ldx >= rows, i.e. X as ojbkq_dequant_matmul and ojbkq_quantize_layer take
+ *   it, with `rows` tokens; block_rows must be 1 then.
+ *   X8, scales: the 8-bit array [rows, m]; bytes m .. of a row up to m rounded
+ *   up to 16 are zeroed.
+ *   rows >= 1, 1 <= m <= 2^20, rows <= 2^24, block_rows 1 or 128.           */
+int ojbkq_quantize_fp8(const void* X, int32_t xtype, int64_t rows, int64_t m, int64_t ldx,
+                       int32_t features_first, int32_t block_rows, uint8_t* X8, int64_t ld8,
+                       uint8_t* scales, int64_t lds, void* stream);
+
+/* Root-mean-square norm of a residual stream, its output in 8 bits:
+ *     h = x + residual_in (a float32 sum; h = x where residual_in is NULL),
+ *     residual_out = h rounded to rtype,
+ *     y = h gain / sqrt(mean(h^2) + eps)   (the mean over the token's features),
+ *   and y is brought to 8 bits as by ojbkq_quantize_fp8 with block_rows = 1.
+ *   Norm and rounding to 8 bits are those of float64 (y is not rounded in
+ *   between); a y beyond float32's range counts as infinite.  A token whose h
+ *   holds a NaN or an infinity comes out as NaN, and so does one of zeros with
+ *   eps = 0 (0 / 0).
+ *   x [T, m] type xtype, row stride ldx; residual_in, residual_out [T, m] type
+ *   rtype, row stride ldr (elements), both or neither given; they may be the
+ *   same array (an update in place) and otherwise must not overlap, nor may
+ *   residual_out overlap x.  gain [m] float32 (NULL: 1).  eps >= 0, finite.
+ *   X8, scales as above.  T >= 1, 1 <= m <= 2^20, T <= 2^24.                */
+int ojbkq_rmsnorm_fp8(const void* x, int32_t xtype, int64_t T, int64_t m, int64_t ldx,
+                      const void* residual_in, void* residual_out, int32_t rtype, int64_t ldr,
+                      const float* gain, double eps, uint8_t* X8, int64_t ld8, uint8_t* scales,
+                      int64_t lds, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* OJBKQ_FP8_H */

@@ -1,7 +1,7 @@
 """MI355X (gfx950) implementation of OJBKQ's per-layer quantisation path.
 
-A thin Python binding over the C ABI of ``include/ojbkq.h`` (``libojbkq.so``
-in this directory).  Only argument marshalling happens here: torch supplies
+A thin Python binding over the C ABI of ``include/ojbkq.h`` and
+``include/ojbkq_fp8.h`` (``libojbkq.so`` in this directory).  Only argument marshalling happens here: torch supplies
 device memory and the current stream, every step of the path runs in the HIP
 kernels of the library.  There is no fallback: without the built library
 every call raises.
@@ -20,7 +20,7 @@ import torch
 __all__ = [
     "OjbkqError", "Params", "library", "library_path", "quantize_layer", "LayerSolver",
     "decode_stage", "klein_log_rho", "workspace_bytes", "decode_workspace_bytes",
-    "ABI_FUNCTIONS", "QuantResult", "STAGES",
+    "ABI_FUNCTIONS", "QuantResult", "STAGES", "FP8_FUNCTIONS", "quantize_fp8", "rmsnorm_fp8",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -36,6 +36,9 @@ ABI_FUNCTIONS = (
     "ojbkq_quantize_layer_noalloc", "ojbkq_dequant_matmul_workspace_bytes",
     "ojbkq_dequant_matmul_ws",
 )
+
+# every entry point of include/ojbkq_fp8.h
+FP8_FUNCTIONS = ("ojbkq_quantize_fp8", "ojbkq_rmsnorm_fp8")
 
 NOALLOC_SCRATCH_BYTES = 256 * 1024 * 1024   # OJBKQ_NOALLOC_SCRATCH_BYTES
 
@@ -76,6 +79,7 @@ def library() -> ctypes.CDLL:
                            "`python -m paper_2602_08376_amd.build` (no CPU fallback exists)")
     lib = ctypes.CDLL(library_path)
     P, vp, i64, dp = ctypes.POINTER(Params), ctypes.c_void_p, ctypes.c_int64, ctypes.c_double
+    i32 = ctypes.c_int32
     sig = {
         "ojbkq_workspace_bytes": (ctypes.c_size_t, [P]),
         "ojbkq_decode_workspace_bytes": (ctypes.c_size_t, [P]),
@@ -105,6 +109,10 @@ def library() -> ctypes.CDLL:
         "ojbkq_set_timing": (ctypes.c_int, [vp, ctypes.c_int]),
         "ojbkq_stage_times": (ctypes.c_int, [vp, ctypes.POINTER(ctypes.c_double)]),
         "ojbkq_last_error": (ctypes.c_char_p, []),
+        "ojbkq_quantize_fp8": (ctypes.c_int, [vp, i32, i64, i64, i64, i32, i32, vp, i64, vp, i64,
+                                              vp]),
+        "ojbkq_rmsnorm_fp8": (ctypes.c_int, [vp, i32, i64, i64, i64, vp, vp, i32, i64, vp, dp, vp,
+                                             i64, vp, i64, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -527,3 +535,125 @@ def dequant_matmul(packed: torch.Tensor, scales: torch.Tensor, zeros: torch.Tens
                                              _ptr(Y), T, _ptr(ws), ws.numel(), _stream(dev)))
     return Y
 
+
+
+# ---------------------------------------------------------------------------
+# activations in 8 bits: e4m3 values with a power-of-two (e8m0) scale for each
+# block of 128 features
+# ---------------------------------------------------------------------------
+
+FP8_BLOCK = 128                                    # OJBKQ_FP8_BLOCK
+E4M3, E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+FP8_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}   # OJBKQ_F32, _F16, _BF16
+
+
+class _device:
+    """The device of the call's tensors made the current one, where it is not."""
+
+    def __init__(self, dev):
+        self.dev, self.back = dev.index, None
+
+    def __enter__(self):
+        here = torch.cuda.current_device()
+        if here != self.dev:
+            torch.cuda.set_device(self.dev)
+            self.back = here
+
+    def __exit__(self, *exc):
+        if self.back is not None:
+            torch.cuda.set_device(self.back)
+
+
+def _up(v: int, step: int) -> int:
+    return -(-v // step) * step
+
+
+def _matrix(t, name, types, shape=None, device=None):
+    """(rows, columns, row stride) of a 2-D GPU tensor with contiguous rows."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype not in types:
+        raise ValueError(f"{name} must be one of {', '.join(map(str, types))} (got {t.dtype})")
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name} must be a matrix{'' if shape is None else ' of shape ' + str(tuple(shape))} "
+                         f"(got {tuple(t.shape)})")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be on the GPU (got {t.device})")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} rows must be contiguous")
+    ld = t.stride(0) if rows > 1 else cols
+    if rows > 1 and ld < cols:
+        raise ValueError(f"{name} rows must not overlap")
+    return rows, cols, ld
+
+
+def _fp8_empty(rows, m, block_rows, dev):
+    """Uninitialised 8-bit array [rows, m] and its scales, rows padded to whole
+    blocks of 128 values and to four scales."""
+    G = -(-m // FP8_BLOCK)
+    v = torch.empty(rows, G * FP8_BLOCK, dtype=E4M3, device=dev)
+    s = torch.empty(-(-rows // block_rows), _up(G, 4), dtype=E8M0, device=dev)
+    return v[:, :m], s[:, :G]
+
+
+def quantize_fp8(X: torch.Tensor, block_rows: int = 1, features_first: bool = False):
+    """``ojbkq_quantize_fp8``: X brought to 8 bits, (values, scales) with values
+    [rows, m] float8_e4m3fn and scales [ceil(rows / block_rows), ceil(m / 128)]
+    float8_e8m0fnu, value x scale standing for X.
+
+    X float32, float16 or bfloat16 with contiguous rows: [rows, m], or with
+    ``features_first`` [m, rows] (activations as ``dequant_matmul`` takes them).
+    ``block_rows``: 1 (a scale to 128 features of a row: activations) or 128 (to
+    128 rows x 128 features: weights).  Both results keep their rows padded (to
+    128 values, to four scales), as the products need them; slices of their
+    rows are as good as they are."""
+    a, b, ld = _matrix(X, "X", FP8_TYPES)
+    rows, m = (b, a) if features_first else (a, b)
+    if block_rows not in (1, 128):
+        raise ValueError("block_rows must be 1 or 128")
+    dev = X.device
+    with _device(dev):
+        v, s = _fp8_empty(rows, m, block_rows, dev)
+        _check(library().ojbkq_quantize_fp8(_ptr(X), FP8_TYPES[X.dtype], rows, m, ld,
+                                            1 if features_first else 0, block_rows, _ptr(v),
+                                            _up(m, FP8_BLOCK), _ptr(s), _up(s.shape[1], 4),
+                                            _stream(dev)))
+    return v, s
+
+
+def rmsnorm_fp8(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float,
+                residual: Optional[torch.Tensor] = None,
+                residual_out: Optional[torch.Tensor] = None):
+    """``ojbkq_rmsnorm_fp8``: (values, scales) of h gain / sqrt(mean(h^2) + eps)
+    with h = x + residual, in 8 bits as by :func:`quantize_fp8`.
+
+    x [T, m] float32, float16 or bfloat16; gain [m] float32 or None; residual
+    [T, m] of any of these types or None.  The residual stream becomes h,
+    rounded to its type: in place, or in ``residual_out`` (the residual's type
+    and strides)."""
+    T, m, ldx = _matrix(x, "x", FP8_TYPES)
+    dev = x.device
+    if gain is not None:
+        _need(gain, "gain", torch.float32, (m,), dev)
+        if not gain.is_contiguous():
+            raise ValueError("gain must be contiguous")
+    rtype, ldr = 0, m
+    if residual is not None:
+        _, _, ldr = _matrix(residual, "residual", FP8_TYPES, (T, m), dev)
+        rtype = FP8_TYPES[residual.dtype]
+        if residual_out is None:
+            residual_out = residual
+        elif _matrix(residual_out, "residual_out", (residual.dtype,), (T, m), dev)[2] != ldr:
+            raise ValueError("residual_out must have the strides of residual")
+    elif residual_out is not None:
+        raise ValueError("residual_out needs a residual")
+    with _device(dev):
+        v, s = _fp8_empty(T, m, 1, dev)
+        _check(library().ojbkq_rmsnorm_fp8(_ptr(x), FP8_TYPES[x.dtype], T, m, ldx, _ptr(residual),
+                                           _ptr(residual_out), rtype, ldr, _ptr(gain), float(eps),
+                                           _ptr(v), _up(m, FP8_BLOCK), _ptr(s),
+                                           _up(s.shape[1], 4), _stream(dev)))
+    return v, s

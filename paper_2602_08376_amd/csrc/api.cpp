@@ -13,11 +13,14 @@
 #include <utility>
 #include <vector>
 
+#include "api_error.h"
 #include "kernels.h"
 
-namespace {
+namespace ojbkq {
 
-thread_local std::string g_error;
+static thread_local std::string g_error;
+
+void clear_error() { g_error.clear(); }
 
 int fail(int code, const std::string& msg) {
   g_error = msg;
@@ -28,11 +31,12 @@ int hip_fail(hipError_t e, const char* where) {
   return fail(OJBKQ_EHIP, std::string(where) + ": " + hipGetErrorString(e));
 }
 
-#define OJBKQ_HIP(call, where)                     \
-  do {                                             \
-    hipError_t e_ = (call);                        \
-    if (e_ != hipSuccess) return hip_fail(e_, where); \
-  } while (0)
+}  // namespace ojbkq
+
+namespace {
+
+using ojbkq::fail;
+using ojbkq::g_error;
 
 constexpr size_t kAlign = 256;
 constexpr int kStatusClear = 0x7f7f7f7f;   // byte-fill value meaning "no bad pivot"

@@ -1,0 +1,173 @@
+// Root-mean-square norm of a residual stream with its output in 8 bits
+// (ojbkq_rmsnorm_fp8).
+#include "fp8_pack.h"
+
+namespace ojbkq {
+namespace {
+
+struct None {};   // no residual
+
+template <class E>
+__device__ __forceinline__ void widen(const Eight<E>& x, float (&h)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) h[e] = (float)x.v[e];
+}
+
+// One workgroup of NT threads to a token.  A thread holds NV runs of eight
+// neighbouring features of h in registers (NT * 8 * NV >= m), so x and the
+// residual are read once: bound by memory.  The squares are summed in float64
+// (no finite h overflows), and y is formed and rounded from float64, which
+// costs no more than float32 here: the vector ALU does 64-bit products at the
+// rate of 32-bit ones, and memory leaves it about 70 operations an element.
+// NV = 0: longer rows, read twice.
+template <int XT, int RT, int NT, int NV>
+__global__ __launch_bounds__(NT) void rmsnorm_kernel(Norm8Args a) {
+  typedef typename Number<XT>::type X;
+  typedef typename Number<RT < 0 ? 0 : RT>::type R;
+  constexpr bool kRes = RT >= 0;
+  constexpr int kRuns = NV ? NV : 1, kWaves = NT / 64;
+  __shared__ double part[kWaves];
+  const int tid = threadIdx.x;
+  const int64_t row = blockIdx.x;
+  const X* const x = static_cast<const X*>(a.x) + row * a.ldx;
+  const R* const rin = kRes ? static_cast<const R*>(a.r_in) + row * a.ldr : nullptr;
+  R* const rout = kRes ? static_cast<R*>(a.r_out) + row * a.ldr : nullptr;
+  uint8_t* const dst = a.X8 + row * a.ld8;
+  const int64_t m16 = (a.m + 15) / 16 * 16;
+
+  // h of the eight features from k on (0 past the last one)
+  auto read = [&](int64_t k, float (&h)[8]) {
+    Eight<X> vx;
+    vx.load(x + k, a.m - k);
+    if constexpr (kRes) {
+      Eight<R> vr;
+      vr.load(rin + k, a.m - k);
+      float r[8];
+      widen(vr, r);
+      widen(vx, h);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[e] += r[e];
+    } else {
+      widen(vx, h);
+    }
+  };
+  auto squares = [&](const float (&h)[8]) {
+    double s = 0.0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = __builtin_fma((double)h[e], (double)h[e], s);
+    return s;
+  };
+  // the token's sum, in every thread
+  auto total = [&](double s) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d);
+    if constexpr (kWaves > 1) {
+      if ((tid & 63) == 0) part[tid >> 6] = s;
+      __syncthreads();
+      s = 0.0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) s += part[w];
+    }
+    return s;
+  };
+  auto finish = [&](int64_t k, const float (&h)[8], double inv) {
+    if constexpr (kRes) {
+      Eight<R> o;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o.v[e] = (R)h[e];
+      o.store(rout + k, a.m - k);
+    }
+    float g[8];
+    if (a.gain) {
+      Eight<float> vg;
+      vg.load(a.gain + k, a.m - k);
+      widen(vg, g);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) g[e] = 1.f;
+    }
+    uint32_t hi[8], most = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      // (inv is NaN for a token with one; past the last feature h is 0)
+      hi[e] = k + e < a.m ? sticky_high((double)h[e] * inv * (double)g[e]) : 0u;
+      const uint32_t s = size_key64(hi[e]);
+      most = most > s ? most : s;
+    }
+    const uint32_t code = scale_code64(max16(most));
+    if (k < m16) *reinterpret_cast<u2*>(dst + k) = to_e4m3(hi, code);
+    if ((tid & 15) == 0 && k < a.m) a.scales[row * a.lds + (k >> 7)] = (uint8_t)code;
+  };
+  // infinite sums (an infinity in h) give NaN for the whole token
+  auto inverse = [&](double s) {
+    return s < __builtin_huge_val() ? 1.0 / __builtin_sqrt(s / (double)a.m + a.eps)
+                                    : __builtin_nan("");
+  };
+
+  if constexpr (NV > 0) {
+    float h[kRuns][8];
+#pragma unroll
+    for (int i = 0; i < kRuns; ++i) read(8 * ((int64_t)tid + NT * i), h[i]);
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < kRuns; ++i) s += squares(h[i]);
+    const double inv = inverse(total(s));
+#pragma unroll
+    for (int i = 0; i < kRuns; ++i) finish(8 * ((int64_t)tid + NT * i), h[i], inv);
+  } else {
+    // every thread reads the same features both times, so the residual may be
+    // updated in place
+    double s = 0.0;
+    float h[8];
+    const int64_t whole = (a.m + 127) / 128 * 128;   // whole rows of 16 lanes for max16
+    for (int64_t k = 8 * tid; k < a.m; k += 8 * NT) {
+      read(k, h);
+      s += squares(h);
+    }
+    const double inv = inverse(total(s));
+    for (int64_t k = 8 * tid; k < whole; k += 8 * NT) {
+      read(k, h);
+      finish(k, h, inv);
+    }
+  }
+}
+
+template <int XT, int RT>
+hipError_t launch(const Norm8Args& a, hipStream_t s) {
+  const dim3 grid((unsigned)a.T);
+#define OJBKQ_NORM(NT, NV) rmsnorm_kernel<XT, RT, NT, NV><<<grid, dim3(NT), 0, s>>>(a)
+  // few tokens leave CUs idle: many threads to each, for latency; otherwise
+  // few threads with several loads each under way
+  if (a.m <= 2048) OJBKQ_NORM(256, 1);
+  else if (a.m <= 8192 && a.T <= 512) OJBKQ_NORM(1024, 1);
+  else if (a.m <= 4096) OJBKQ_NORM(256, 2);
+  else if (a.m <= 8192) OJBKQ_NORM(256, 4);
+  else if (a.m <= 32768) OJBKQ_NORM(1024, 4);
+  else OJBKQ_NORM(1024, 0);
+#undef OJBKQ_NORM
+  return hipGetLastError();
+}
+
+template <int XT>
+hipError_t launch_x(const Norm8Args& a, int rtype, hipStream_t s) {
+  if (!a.r_in) return launch<XT, -1>(a, s);
+  switch (rtype) {
+    case 0: return launch<XT, 0>(a, s);
+    case 1: return launch<XT, 1>(a, s);
+    case 2: return launch<XT, 2>(a, s);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_rmsnorm_fp8(const Norm8Args& a, int xtype, int rtype, hipStream_t stream) {
+  switch (xtype) {
+    case 0: return launch_x<0>(a, rtype, stream);
+    case 1: return launch_x<1>(a, rtype, stream);
+    case 2: return launch_x<2>(a, rtype, stream);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace ojbkq
