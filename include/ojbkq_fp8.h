@@ -84,6 +84,45 @@ int ojbkq_rmsnorm_fp8(const void* x, int32_t xtype, int64_t T, int64_t m, int64_
                       const float* gain, double eps, uint8_t* X8, int64_t ld8, uint8_t* scales,
                       int64_t lds, void* stream);
 
+/* The product of 8-bit weights with 8-bit activations:
+ *     Y[j][t] = sum over blocks g of  sw[j / r][g] sx[t][g] sum_i W8[j][i] X8[t][i],
+ *   i over the features of block g and r = w_block_rows (1 or 128).
+ *   W8 [n, m] e4m3, row stride ldw; w_scales [ceil(n / r), ceil(m / 128)],
+ *   row stride ldws (elements), any OJBKQ_SCALE_F32 or OJBKQ_SCALE_E8M0: with
+ *   e8m0 ones an 8-bit array as above (ojbkq_quantize_fp8 of W).
+ *   X8 [T, m] with scales x_scales: an 8-bit array of block_rows = 1.
+ *   Y: type ytype; tokens_first = 0: [n, T], row stride ldy >= T, as
+ *   ojbkq_dequant_matmul gives it; tokens_first = 1: [T, n], ldy >= n.
+ *   Results are rounded to ytype once.
+ *   A NaN in a token or a channel comes out in all it meets; so does an
+ *   infinite scale.  n, T in [1, 2^24], m in [1, 2^20].                     */
+int ojbkq_matmul_fp8(const uint8_t* W8, int64_t ldw, const void* w_scales, int32_t w_scale_type,
+                     int32_t w_block_rows, int64_t ldws, int64_t n, int64_t m, const uint8_t* X8,
+                     int64_t ldx, const uint8_t* x_scales, int64_t ldxs, int64_t T, void* Y,
+                     int32_t ytype, int32_t tokens_first, int64_t ldy, void* stream);
+
+/* The product of a layer as this library quantizes it (packed, scales, zeros,
+ * bits and group as in ojbkq_dequant_matmul, without a permutation) with 8-bit
+ * activations:
+ *     Y[j][t] = sum over groups g of  s[j][g] sum_i (q[j][i] - z[j][g]) X[t][i],
+ *   X[t][i] = X8[t][i] sx[t][i / 128].  A code less its zero point is a whole
+ *   number of at most 15 and enters the products exactly; no weight is rounded.
+ *   bits in [1, 4]; group a multiple of 128, or one group (group <= 0 or >= m).
+ *   zeros are whole numbers in 0 .. 2^bits - 1, as the quantize calls return
+ *   them (any other is taken as the nearest of these).
+ *   X8, x_scales, Y, ytype, tokens_first, ldy as in ojbkq_matmul_fp8.
+ *   workspace: ojbkq_dequant_matmul_fp8_workspace_bytes(n, m, T) bytes, 16-byte
+ *   aligned (NULL where that is 0), untouched until the product has run:
+ *   ENOSPACE for fewer, EINVAL for a NULL or misaligned one.
+ * ojbkq_dequant_matmul_fp8_workspace_bytes: host-only; 0 for sizes that need
+ *   none, and for those that the product rejects.                           */
+size_t ojbkq_dequant_matmul_fp8_workspace_bytes(int64_t n, int64_t m, int64_t T);
+int ojbkq_dequant_matmul_fp8(const uint32_t* packed, const float* scales, const float* zeros,
+                             int64_t n, int64_t m, int32_t bits, int32_t group, const uint8_t* X8,
+                             int64_t ldx, const uint8_t* x_scales, int64_t ldxs, int64_t T,
+                             void* Y, int32_t ytype, int32_t tokens_first, int64_t ldy,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,6 +21,7 @@ __all__ = [
     "OjbkqError", "Params", "library", "library_path", "quantize_layer", "LayerSolver",
     "decode_stage", "klein_log_rho", "workspace_bytes", "decode_workspace_bytes",
     "ABI_FUNCTIONS", "QuantResult", "STAGES", "FP8_FUNCTIONS", "quantize_fp8", "rmsnorm_fp8",
+    "matmul_fp8", "dequant_matmul_fp8",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -38,7 +39,8 @@ ABI_FUNCTIONS = (
 )
 
 # every entry point of include/ojbkq_fp8.h
-FP8_FUNCTIONS = ("ojbkq_quantize_fp8", "ojbkq_rmsnorm_fp8")
+FP8_FUNCTIONS = ("ojbkq_quantize_fp8", "ojbkq_rmsnorm_fp8", "ojbkq_matmul_fp8",
+                 "ojbkq_dequant_matmul_fp8", "ojbkq_dequant_matmul_fp8_workspace_bytes")
 
 NOALLOC_SCRATCH_BYTES = 256 * 1024 * 1024   # OJBKQ_NOALLOC_SCRATCH_BYTES
 
@@ -113,6 +115,12 @@ def library() -> ctypes.CDLL:
                                               vp]),
         "ojbkq_rmsnorm_fp8": (ctypes.c_int, [vp, i32, i64, i64, i64, vp, vp, i32, i64, vp, dp, vp,
                                              i64, vp, i64, vp]),
+        "ojbkq_matmul_fp8": (ctypes.c_int, [vp, i64, vp, i32, i32, i64, i64, i64, vp, i64, vp, i64,
+                                            i64, vp, i32, i32, i64, vp]),
+        "ojbkq_dequant_matmul_fp8_workspace_bytes": (ctypes.c_size_t, [i64, i64, i64]),
+        "ojbkq_dequant_matmul_fp8": (ctypes.c_int, [vp, vp, vp, i64, i64, i32, i32, vp, i64, vp,
+                                                    i64, i64, vp, i32, i32, i64, vp,
+                                                    ctypes.c_size_t, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -657,3 +665,116 @@ def rmsnorm_fp8(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float,
                                            _ptr(v), _up(m, FP8_BLOCK), _ptr(s),
                                            _up(s.shape[1], 4), _stream(dev)))
     return v, s
+
+
+def _room(t, last):
+    """Whether t's storage holds `last` elements from its first one on."""
+    return t.storage_offset() + last <= t.untyped_storage().nbytes() // t.element_size()
+
+
+def _fp8_values(v, name, dev=None):
+    """(rows, m, row stride) of an 8-bit array's values, laid out as the
+    products need them."""
+    rows, m, ld = _matrix(v, name, (E4M3,), device=dev)
+    m16 = _up(m, 16)
+    if rows == 1:
+        ld = m16
+    if ld % 16 or ld < m16 or v.data_ptr() % 16 or not _room(v, (rows - 1) * ld + m16):
+        raise ValueError(f"{name} needs 16-byte aligned rows that are readable up to a multiple of 16 "
+                         "values, as quantize_fp8 returns them")
+    return rows, m, ld
+
+
+def _fp8_scales(s, name, shape, dev):
+    """Row stride of an 8-bit array's e8m0 scales, laid out likewise."""
+    rows, G, ld = _matrix(s, name, (E8M0,), shape, dev)
+    if rows == 1:
+        ld = _up(G, 4)
+    if ld % 4 or ld < _up(G, 4) or s.data_ptr() % 4 or not _room(s, (rows - 1) * ld + _up(G, 4)):
+        raise ValueError(f"{name} needs 4-byte aligned rows that are readable up to a multiple of 4 "
+                         "scales, as quantize_fp8 returns them")
+    return ld
+
+
+def _result(n, T, tokens_first, dtype, dev):
+    if dtype not in FP8_TYPES:
+        raise ValueError(f"dtype must be one of {', '.join(map(str, FP8_TYPES))} (got {dtype})")
+    return torch.empty((T, n) if tokens_first else (n, T), dtype=dtype, device=dev)
+
+
+def matmul_fp8(W8: torch.Tensor, w_scales: torch.Tensor, X8: torch.Tensor, x_scales: torch.Tensor,
+               tokens_first: bool = False, dtype=torch.float32) -> torch.Tensor:
+    """``ojbkq_matmul_fp8``: Y = W X of 8-bit weights and activations, each value
+    times its block's scale.
+
+    W8 [n, m] float8_e4m3fn with w_scales [ceil(n / 128), ceil(m / 128)] or [n,
+    ceil(m / 128)], float8_e8m0fnu (both from :func:`quantize_fp8`) or float32;
+    X8 [T, m] and x_scales from :func:`quantize_fp8` or :func:`rmsnorm_fp8`.
+    Returns [n, T] as :func:`dequant_matmul` does, or [T, n] with
+    ``tokens_first``, in ``dtype`` (float32, float16 or bfloat16)."""
+    T, m, ldx = _fp8_values(X8, "X8")
+    dev, G = X8.device, -(-m // FP8_BLOCK)
+    ldxs = _fp8_scales(x_scales, "x_scales", (T, G), dev)
+    n, mw, ldw = _fp8_values(W8, "W8", dev)
+    if mw != m:
+        raise ValueError(f"W8 has {mw} features and X8 {m}")
+    rows = w_scales.shape[0] if w_scales.dim() == 2 else -1
+    if rows not in (n, -(-n // FP8_BLOCK)):
+        raise ValueError(f"w_scales must have a row for each row or for each 128 rows of W8 (got {rows})")
+    e8m0 = w_scales.dtype == E8M0
+    if e8m0:
+        ldws = _fp8_scales(w_scales, "w_scales", (rows, G), dev)
+    else:
+        ldws = _matrix(w_scales, "w_scales", (torch.float32, E8M0), (rows, G), dev)[2]
+    with _device(dev):
+        Y = _result(n, T, tokens_first, dtype, dev)
+        _check(library().ojbkq_matmul_fp8(_ptr(W8), ldw, _ptr(w_scales), 1 if e8m0 else 0,
+                                          1 if rows == n else 128, ldws, n, m, _ptr(X8), ldx,
+                                          _ptr(x_scales), ldxs, T, _ptr(Y), FP8_TYPES[dtype],
+                                          1 if tokens_first else 0, Y.shape[1], _stream(dev)))
+    return Y
+
+
+def dequant_matmul_fp8(packed: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor, m: int,
+                       bits: int, group: int, X8: torch.Tensor, x_scales: torch.Tensor,
+                       tokens_first: bool = False, dtype=torch.float32,
+                       workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``ojbkq_dequant_matmul_fp8``: Y = S (Q - Z) X of a layer quantized by this
+    package (packed codes of at most 4 bits, groups of a multiple of 128
+    features or one) with 8-bit activations X8 [T, m], x_scales from
+    :func:`quantize_fp8` or :func:`rmsnorm_fp8`.
+
+    Returns [n, T], or [T, n] with ``tokens_first``, in ``dtype``.
+    ``workspace``: a uint8 device tensor of
+    ``ojbkq_dequant_matmul_fp8_workspace_bytes`` bytes (allocated here when
+    None and needed)."""
+    T, mx, ldx = _fp8_values(X8, "X8")
+    m, dev = int(m), X8.device
+    if mx != m:
+        raise ValueError(f"X8 has {mx} features, expected {m}")
+    ldxs = _fp8_scales(x_scales, "x_scales", (T, -(-m // FP8_BLOCK)), dev)
+    n = packed.shape[0]
+    _need(packed, "packed", torch.int32, (n, packed_words(m, bits)), dev)
+    group = 0 if group >= m else int(group)
+    G = num_groups(m, group)
+    _need(scales, "scales", torch.float32, (n, G), dev)
+    _need(zeros, "zeros", torch.float32, (n, G), dev)
+    if not (packed.is_contiguous() and scales.is_contiguous() and zeros.is_contiguous()):
+        raise ValueError("packed, scales and zeros must be contiguous")
+    lib = library()
+    need = int(lib.ojbkq_dequant_matmul_fp8_workspace_bytes(n, m, T))
+    with _device(dev):
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        else:
+            _need(workspace, "workspace", torch.uint8, device=dev)
+            if not workspace.is_contiguous():
+                raise ValueError("workspace must be contiguous")
+        Y = _result(n, T, tokens_first, dtype, dev)
+        _check(lib.ojbkq_dequant_matmul_fp8(_ptr(packed), _ptr(scales), _ptr(zeros), n, m,
+                                            int(bits), group, _ptr(X8), ldx, _ptr(x_scales),
+                                            ldxs, T, _ptr(Y), FP8_TYPES[dtype],
+                                            1 if tokens_first else 0, Y.shape[1], _ptr(workspace),
+                                            0 if workspace is None else workspace.numel(),
+                                            _stream(dev)))
+    return Y

@@ -22,7 +22,7 @@ LIB = os.path.join(PKG, "libojbkq.so")
 
 SOURCES = ["api.cpp", "gemm.hip", "gram.hip", "gram_i8.hip", "factor.hip", "chol_dag.hip", "quant.hip", "decode.hip",
            "infer.hip", "infer_few.hip", "permute.hip", "noalloc.hip",
-           "api_fp8.cpp", "fp8_quantize.hip", "fp8_norm.hip"]
+           "api_fp8.cpp", "fp8_quantize.hip", "fp8_norm.hip", "fp8_few.hip", "fp8_matmul.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",

@@ -6,6 +6,7 @@
 
 #include "api_error.h"
 #include "fp8.h"
+#include "kernels.h"
 
 namespace {
 
@@ -31,6 +32,25 @@ int check_fp8(const char* name, const void* X8, int64_t ld8, const void* scales,
   if (misaligned(X8, 16) || misaligned(scales, 4))
     return fail(OJBKQ_EINVAL, n + " must be 16-byte aligned and its scales 4-byte aligned");
   return OJBKQ_OK;
+}
+
+bool product_sizes_ok(int64_t n, int64_t m, int64_t T) {
+  return n >= 1 && m >= 1 && T >= 1 && n <= kMaxRows && T <= kMaxRows && m <= kMaxFeatures;
+}
+
+// What both products share: sizes, activations, result.
+int check_product(int64_t n, int64_t m, int64_t T, const uint8_t* X8, int64_t ldx,
+                  const uint8_t* x_scales, int64_t ldxs, const void* Y, int32_t ytype,
+                  int32_t tokens_first, int64_t ldy) {
+  if (!Y) return fail(OJBKQ_EINVAL, "Y is required");
+  if (!product_sizes_ok(n, m, T))
+    return fail(OJBKQ_EINVAL, "n and T must be in [1, 2^24] and m in [1, 2^20]");
+  if (!type_ok(ytype)) return fail(OJBKQ_EINVAL, "ytype must be OJBKQ_F32, OJBKQ_F16 or OJBKQ_BF16");
+  if (tokens_first != 0 && tokens_first != 1) return fail(OJBKQ_EINVAL, "tokens_first must be 0 or 1");
+  if (ldy < (tokens_first ? n : T) || ldy > kMaxStride)
+    return fail(OJBKQ_EINVAL, "ldy must be at least the length of Y's rows");
+  if (misaligned(Y, size_of(ytype))) return fail(OJBKQ_EINVAL, "Y must be aligned to its type");
+  return check_fp8("X8", X8, ldx, x_scales, ldxs, m);
 }
 
 }  // namespace
@@ -85,6 +105,67 @@ int ojbkq_rmsnorm_fp8(const void* x, int32_t xtype, int64_t T, int64_t m, int64_
   const ojbkq::Norm8Args a{x, T, m, ldx, residual_in, residual_out, ldr, gain, eps, X8, ld8, scales, lds};
   OJBKQ_HIP(ojbkq::launch_rmsnorm_fp8(a, xtype, rtype, static_cast<hipStream_t>(stream)),
             "rms norm to 8 bits");
+  return OJBKQ_OK;
+}
+
+int ojbkq_matmul_fp8(const uint8_t* W8, int64_t ldw, const void* w_scales, int32_t w_scale_type,
+                     int32_t w_block_rows, int64_t ldws, int64_t n, int64_t m, const uint8_t* X8,
+                     int64_t ldx, const uint8_t* x_scales, int64_t ldxs, int64_t T, void* Y,
+                     int32_t ytype, int32_t tokens_first, int64_t ldy, void* stream) {
+  ojbkq::clear_error();
+  if (int rc = check_product(n, m, T, X8, ldx, x_scales, ldxs, Y, ytype, tokens_first, ldy)) return rc;
+  if (w_scale_type != OJBKQ_SCALE_F32 && w_scale_type != OJBKQ_SCALE_E8M0)
+    return fail(OJBKQ_EINVAL, "w_scale_type must be OJBKQ_SCALE_F32 or OJBKQ_SCALE_E8M0");
+  if (w_block_rows != 1 && w_block_rows != 128) return fail(OJBKQ_EINVAL, "w_block_rows must be 1 or 128");
+  const bool e8m0 = w_scale_type == OJBKQ_SCALE_E8M0;
+  const int64_t G = (m + OJBKQ_FP8_BLOCK - 1) / OJBKQ_FP8_BLOCK;
+  if (int rc = check_fp8("W8", W8, ldw, w_scales, e8m0 ? ldws : (G + 3) / 4 * 4, m)) return rc;
+  if (!e8m0 && (ldws < G || ldws > kMaxStride)) return fail(OJBKQ_EINVAL, "ldws must be >= ceil(m / 128)");
+  ojbkq::Product8Args a{};
+  a.n = n; a.m = m; a.T = T;
+  a.W8 = W8; a.ldw = ldw;
+  a.ws = w_scales; a.ws_ld = ldws; a.ws_shift = w_block_rows == 128 ? 7 : 0; a.ws_e8m0 = e8m0; a.ws_div = 1;
+  a.X8 = X8; a.ldx = ldx; a.xs = x_scales; a.lds = ldxs;
+  a.Y = Y; a.ldy = ldy; a.ytype = ytype; a.tokens_first = tokens_first;
+  OJBKQ_HIP(ojbkq::launch_product8(a, 0, nullptr, static_cast<hipStream_t>(stream)), "8-bit product");
+  return OJBKQ_OK;
+}
+
+size_t ojbkq_dequant_matmul_fp8_workspace_bytes(int64_t n, int64_t m, int64_t T) {
+  return product_sizes_ok(n, m, T) ? ojbkq::product8_workspace_bytes(n, m, T) : 0;
+}
+
+int ojbkq_dequant_matmul_fp8(const uint32_t* packed, const float* scales, const float* zeros,
+                             int64_t n, int64_t m, int32_t bits, int32_t group, const uint8_t* X8,
+                             int64_t ldx, const uint8_t* x_scales, int64_t ldxs, int64_t T,
+                             void* Y, int32_t ytype, int32_t tokens_first, int64_t ldy,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+  ojbkq::clear_error();
+  if (!packed || !scales || !zeros) return fail(OJBKQ_EINVAL, "packed, scales and zeros are required");
+  if (misaligned(packed, 4) || misaligned(scales, 4) || misaligned(zeros, 4))
+    return fail(OJBKQ_EINVAL, "packed, scales and zeros must be aligned to their types");
+  if (int rc = check_product(n, m, T, X8, ldx, x_scales, ldxs, Y, ytype, tokens_first, ldy)) return rc;
+  if (bits < 1 || bits > 4)
+    return fail(OJBKQ_EINVAL, "bits must be in [1, 4]: longer codes are not exact in 8-bit floating point");
+  const int64_t g = (group <= 0 || group >= m) ? m : group;
+  if (g != m && g % OJBKQ_FP8_BLOCK != 0)
+    return fail(OJBKQ_EINVAL, "the group must be a multiple of 128 (or the whole column)");
+  const size_t need = ojbkq::product8_workspace_bytes(n, m, T);
+  if (need) {
+    if (!workspace) return fail(OJBKQ_EINVAL, "this product needs a workspace");
+    if (workspace_bytes < need)
+      return fail(OJBKQ_ENOSPACE, "workspace smaller than ojbkq_dequant_matmul_fp8_workspace_bytes");
+    if (misaligned(workspace, 16)) return fail(OJBKQ_EINVAL, "the workspace must be 16-byte aligned");
+  }
+  ojbkq::Product8Args a{};
+  a.n = n; a.m = m; a.T = T;
+  a.P = packed; a.wpr = ojbkq::packed_words(m, bits); a.Z = zeros;
+  a.ws = scales; a.ws_ld = (m + g - 1) / g; a.ws_shift = 0; a.ws_e8m0 = 0;
+  a.ws_div = (uint32_t)((g + OJBKQ_FP8_BLOCK - 1) / OJBKQ_FP8_BLOCK);
+  a.X8 = X8; a.ldx = ldx; a.xs = x_scales; a.lds = ldxs;
+  a.Y = Y; a.ldy = ldy; a.ytype = ytype; a.tokens_first = tokens_first;
+  OJBKQ_HIP(ojbkq::launch_product8(a, bits, workspace, static_cast<hipStream_t>(stream)),
+            "product of codes with 8-bit activations");
   return OJBKQ_OK;
 }
 

@@ -41,4 +41,32 @@ struct Norm8Args {
 };
 hipError_t launch_rmsnorm_fp8(const Norm8Args& a, int xtype, int rtype, hipStream_t stream);
 
+// Y = W X^T of 8-bit weights, or of packed codes, with 8-bit activations.
+struct Product8Args {
+  int64_t n, m, T;
+  const uint8_t* W8;      // [n, m] e4m3, row stride ldw; or null:
+  int64_t ldw;
+  const uint32_t* P;      // packed codes, wpr words to a row,
+  int64_t wpr;
+  const float* Z;         // with zero points laid out as the scales
+  const void* ws;         // scale of row j, block b of 128 features:
+  int64_t ws_ld;          //   ws[(j >> ws_shift) * ws_ld + b / ws_div]
+  int ws_shift, ws_e8m0;  //   e8m0 bytes or float32
+  uint32_t ws_div;
+  const uint8_t* X8;      // [T, m] e4m3, row stride ldx, scales xs, row stride lds
+  int64_t ldx;
+  const uint8_t* xs;
+  int64_t lds;
+  void* Y;                // type ytype, tokens_first [T, n] or [n, T], row stride ldy
+  int64_t ldy;
+  int ytype, tokens_first;
+};
+// One pass over the weights or codes for every 64 tokens (fp8_few.hip).
+hipError_t launch_product_few8(const Product8Args& a, int bits, hipStream_t stream);
+// The product in the kernel that its sizes ask for (fp8_matmul.hip); bits = 0:
+// of W8, otherwise of packed codes, with product8_workspace_bytes(n, m, T)
+// bytes of workspace.
+hipError_t launch_product8(const Product8Args& a, int bits, void* workspace, hipStream_t stream);
+size_t product8_workspace_bytes(int64_t n, int64_t m, int64_t T);
+
 }  // namespace ojbkq

@@ -1,0 +1,54 @@
+// What the product kernels with 8-bit operands share (fp8_few.hip,
+// fp8_matmul.hip).
+#pragma once
+
+#include "fp8.h"
+
+namespace ojbkq {
+
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+typedef float v4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+// 2^(code - 127) (code 0: 2^-127, the one below float32's normal range).
+__device__ __forceinline__ float from_e8m0(uint32_t code) {
+  return __uint_as_float(code ? code << 23 : 1u << 22);
+}
+
+// Scale of row j, block b of 128 features of the weights.
+__device__ __forceinline__ float weight_scale(const Product8Args& a, int64_t j, uint32_t b) {
+  const int64_t at = (j >> a.ws_shift) * a.ws_ld + b / a.ws_div;
+  return a.ws_e8m0 ? from_e8m0(static_cast<const uint8_t*>(a.ws)[at])
+                   : static_cast<const float*>(a.ws)[at];
+}
+
+// Eight e4m3 values times a power of two, exactly, in bf16 (whose 8 mantissa
+// bits and float32 exponents hold them).
+__device__ __forceinline__ b8 to_bf16(uint32_t lo, uint32_t hi, float scale) {
+  b8 out;
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    const uint32_t w = h < 2 ? lo : hi;
+    const b2 p = (h & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true)
+                         : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false);
+    out[2 * h] = p.x;
+    out[2 * h + 1] = p.y;
+  }
+  return out;
+}
+
+// The bytes of a word that belong to features below m, the word starting at k.
+__device__ __forceinline__ uint32_t features_below(uint32_t w, int64_t k, int64_t m) {
+  const int64_t left = m - k;
+  return left >= 4 ? w : left <= 0 ? 0u : w & ((1u << (8 * (int)left)) - 1u);
+}
+
+__device__ __forceinline__ void store_y(const Product8Args& a, int64_t j, int64_t t, float v) {
+  const int64_t at = a.tokens_first ? t * a.ldy + j : j * a.ldy + t;
+  if (a.ytype == 0) static_cast<float*>(a.Y)[at] = v;
+  else if (a.ytype == 1) static_cast<_Float16*>(a.Y)[at] = (_Float16)v;
+  else static_cast<__bf16*>(a.Y)[at] = (__bf16)v;
+}
+
+}  // namespace ojbkq
