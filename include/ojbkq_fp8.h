@@ -93,7 +93,15 @@ int ojbkq_rmsnorm_fp8(const void* x, int32_t xtype, int64_t T, int64_t m, int64_
  *   X8 [T, m] with scales x_scales: an 8-bit array of block_rows = 1.
  *   Y: type ytype; tokens_first = 0: [n, T], row stride ldy >= T, as
  *   ojbkq_dequant_matmul gives it; tokens_first = 1: [T, n], ldy >= n.
- *   Results are rounded to ytype once.
+ *   Results are rounded to ytype once.  OJBKQ_F32: products enter exactly and
+ *   are summed in float32.  In 16 bits, the matrix cores' 8-bit products serve
+ *   sizes beyond a few tokens: they add eight neighbouring products after
+ *   cutting each to 13 bits below the largest's leading one (about 1.4e-5 of a
+ *   result's root mean square for Gaussian operands, where rounding to 16 bits
+ *   costs 2e-4 or 1.7e-3), and sums of these in float32.
+ *   Weights and activations (value times scale) are taken as float32's normal
+ *   numbers: a magnitude below 2^-126 may count as 0, one from 2^128 on as
+ *   infinite.
  *   A NaN in a token or a channel comes out in all it meets; so does an
  *   infinite scale.  n, T in [1, 2^24], m in [1, 2^20].                     */
 int ojbkq_matmul_fp8(const uint8_t* W8, int64_t ldw, const void* w_scales, int32_t w_scale_type,

@@ -99,6 +99,15 @@ __global__ __launch_bounds__(512) void product_few8_kernel(Product8Args a) {
     for (int x = 0; x < RB; ++x)
 #pragma unroll
       for (int y = 0; y < NB; ++y) d[x][y] = v4{0.f, 0.f, 0.f, 0.f};
+    float power[RB];
+    if constexpr (SRC == 0) {
+#pragma unroll
+      for (int x = 0; x < RB; ++x) {
+        const SplitScale sp = split_scale(st.s[x]);
+        power[x] = sp.power;
+        st.s[x] = sp.rest;
+      }
+    }
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       b8 fx[NB];
@@ -110,18 +119,12 @@ __global__ __launch_bounds__(512) void product_few8_kernel(Product8Args a) {
       for (int x = 0; x < RB; ++x) {
         b8 fw;
         if constexpr (SRC == 0) {
-          fw = to_bf16(st.w[x][2 * s], st.w[x][2 * s + 1], 1.f);
+          fw = to_bf16(st.w[x][2 * s], st.w[x][2 * s + 1], power[x]);
         } else {
           // (codes past the last one are zero bits; their activations are 0)
-          const float top = (float)((1 << SRC) - 1);
-          const float z = fminf(fmaxf(__builtin_rintf(st.z[x]), 0.f), top);
+          const float z = whole_zero<SRC>(st.z[x]);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int b = (8 * s + e) * SRC, lo = b >> 5, sh = b & 31;
-            uint32_t q = st.w[x][lo] >> sh;
-            if (sh + SRC > 32) q = __builtin_amdgcn_alignbit(st.w[x][lo + 1 < SRC ? lo + 1 : lo], st.w[x][lo], sh);
-            fw[e] = (__bf16)((float)(q & ((1u << SRC) - 1u)) - z);
-          }
+          for (int e = 0; e < 8; ++e) fw[e] = (__bf16)((float)code_of<SRC>(st.w[x], 8 * s + e) - z);
         }
 #pragma unroll
         for (int y = 0; y < NB; ++y)

@@ -23,6 +23,20 @@ __device__ __forceinline__ float weight_scale(const Product8Args& a, int64_t j, 
                    : static_cast<const float*>(a.ws)[at];
 }
 
+// A weight scale as a power of two, which goes to the weights in bf16 or in the
+// matrix instruction (exactly), and the rest, with which a block's sums are
+// multiplied: these then lie in the result's own range, whatever the scales.
+// (0, infinities, NaN and numbers below float32's normal range are all rest.)
+struct SplitScale {
+  float power, rest;
+};
+__device__ __forceinline__ SplitScale split_scale(float s) {
+  const uint32_t b = __float_as_uint(s), e = b & 0x7f800000u;
+  const bool odd = e == 0u || e == 0x7f800000u;
+  return {__uint_as_float(odd ? 0x3f800000u : e),
+          odd ? s : __uint_as_float((b & 0x807fffffu) | 0x3f800000u)};
+}
+
 // Eight e4m3 values times a power of two, exactly, in bf16 (whose 8 mantissa
 // bits and float32 exponents hold them).
 __device__ __forceinline__ b8 to_bf16(uint32_t lo, uint32_t hi, float scale) {
@@ -36,6 +50,20 @@ __device__ __forceinline__ b8 to_bf16(uint32_t lo, uint32_t hi, float scale) {
     out[2 * h + 1] = p.y;
   }
   return out;
+}
+
+// Code c (a constant after unrolling) of 32 that fill BITS words.
+template <int BITS>
+__device__ __forceinline__ uint32_t code_of(const uint32_t (&w)[BITS], int c) {
+  const int b = c * BITS, lo = b >> 5, sh = b & 31;
+  uint32_t q = w[lo] >> sh;
+  if (sh + BITS > 32) q = __builtin_amdgcn_alignbit(w[lo + 1 < BITS ? lo + 1 : lo], w[lo], sh);
+  return q & ((1u << BITS) - 1u);
+}
+// A zero point, the nearest whole number of the codes' range.
+template <int BITS>
+__device__ __forceinline__ float whole_zero(float z) {
+  return fminf(fmaxf(__builtin_rintf(z), 0.f), (float)((1 << BITS) - 1));
 }
 
 // The bytes of a word that belong to features below m, the word starting at k.
