@@ -9,6 +9,7 @@ every call raises.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -555,21 +556,22 @@ E4M3, E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 FP8_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}   # OJBKQ_F32, _F16, _BF16
 
 
-class _device:
+_HERE = contextlib.nullcontext()
+
+
+def _device(dev):
     """The device of the call's tensors made the current one, where it is not."""
+    return _HERE if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
 
-    def __init__(self, dev):
-        self.dev, self.back = dev.index, None
 
-    def __enter__(self):
-        here = torch.cuda.current_device()
-        if here != self.dev:
-            torch.cuda.set_device(self.dev)
-            self.back = here
+def _at(t):
+    return None if t is None else t.data_ptr()
 
-    def __exit__(self, *exc):
-        if self.back is not None:
-            torch.cuda.set_device(self.back)
+
+def _raw_stream(dev):
+    """The current stream's handle (without the Stream object of ``_stream``,
+    which takes as long as a small kernel)."""
+    return torch._C._cuda_getCurrentRawStream(dev.index)
 
 
 def _up(v: int, step: int) -> int:
@@ -582,7 +584,7 @@ def _matrix(t, name, types, shape=None, device=None):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype not in types:
         raise ValueError(f"{name} must be one of {', '.join(map(str, types))} (got {t.dtype})")
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
         raise ValueError(f"{name} must be a matrix{'' if shape is None else ' of shape ' + str(tuple(shape))} "
                          f"(got {tuple(t.shape)})")
     if t.device.type != "cuda":
@@ -602,9 +604,9 @@ def _fp8_empty(rows, m, block_rows, dev):
     """Uninitialised 8-bit array [rows, m] and its scales, rows padded to whole
     blocks of 128 values and to four scales."""
     G = -(-m // FP8_BLOCK)
-    v = torch.empty(rows, G * FP8_BLOCK, dtype=E4M3, device=dev)
-    s = torch.empty(-(-rows // block_rows), _up(G, 4), dtype=E8M0, device=dev)
-    return v[:, :m], s[:, :G]
+    v = torch.empty((rows, G * FP8_BLOCK), dtype=E4M3, device=dev)
+    s = torch.empty((-(-rows // block_rows), _up(G, 4)), dtype=E8M0, device=dev)
+    return v if m % FP8_BLOCK == 0 else v[:, :m], s if G % 4 == 0 else s[:, :G]
 
 
 def quantize_fp8(X: torch.Tensor, block_rows: int = 1, features_first: bool = False):
@@ -625,10 +627,10 @@ def quantize_fp8(X: torch.Tensor, block_rows: int = 1, features_first: bool = Fa
     dev = X.device
     with _device(dev):
         v, s = _fp8_empty(rows, m, block_rows, dev)
-        _check(library().ojbkq_quantize_fp8(_ptr(X), FP8_TYPES[X.dtype], rows, m, ld,
-                                            1 if features_first else 0, block_rows, _ptr(v),
-                                            _up(m, FP8_BLOCK), _ptr(s), _up(s.shape[1], 4),
-                                            _stream(dev)))
+        _check(library().ojbkq_quantize_fp8(_at(X), FP8_TYPES[X.dtype], rows, m, ld,
+                                            1 if features_first else 0, block_rows, _at(v),
+                                            _up(m, FP8_BLOCK), _at(s), _up(s.shape[1], 4),
+                                            _raw_stream(dev)))
     return v, s
 
 
@@ -645,9 +647,8 @@ def rmsnorm_fp8(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float,
     T, m, ldx = _matrix(x, "x", FP8_TYPES)
     dev = x.device
     if gain is not None:
-        _need(gain, "gain", torch.float32, (m,), dev)
-        if not gain.is_contiguous():
-            raise ValueError("gain must be contiguous")
+        if gain.dtype != torch.float32 or gain.shape != (m,) or gain.device != dev or not gain.is_contiguous():
+            raise ValueError(f"gain must be float32 of shape ({m},), contiguous, on {dev}")
     rtype, ldr = 0, m
     if residual is not None:
         _, _, ldr = _matrix(residual, "residual", FP8_TYPES, (T, m), dev)
@@ -660,40 +661,29 @@ def rmsnorm_fp8(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float,
         raise ValueError("residual_out needs a residual")
     with _device(dev):
         v, s = _fp8_empty(T, m, 1, dev)
-        _check(library().ojbkq_rmsnorm_fp8(_ptr(x), FP8_TYPES[x.dtype], T, m, ldx, _ptr(residual),
-                                           _ptr(residual_out), rtype, ldr, _ptr(gain), float(eps),
-                                           _ptr(v), _up(m, FP8_BLOCK), _ptr(s),
-                                           _up(s.shape[1], 4), _stream(dev)))
+        _check(library().ojbkq_rmsnorm_fp8(_at(x), FP8_TYPES[x.dtype], T, m, ldx, _at(residual),
+                                           _at(residual_out), rtype, ldr, _at(gain), float(eps),
+                                           _at(v), _up(m, FP8_BLOCK), _at(s),
+                                           _up(s.shape[1], 4), _raw_stream(dev)))
     return v, s
 
 
-def _room(t, last):
-    """Whether t's storage holds `last` elements from its first one on."""
-    return t.storage_offset() + last <= t.untyped_storage().nbytes() // t.element_size()
-
-
-def _fp8_values(v, name, dev=None):
-    """(rows, m, row stride) of an 8-bit array's values, laid out as the
-    products need them."""
-    rows, m, ld = _matrix(v, name, (E4M3,), device=dev)
-    m16 = _up(m, 16)
+def _padded(t, name, dtype, unit, dev=None, shape=None):
+    """(rows, columns, row stride) of an 8-bit array's values (unit 16) or scales
+    (unit 4): rows aligned to the unit and readable up to a multiple of it."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.dim() != 2 or not t.is_cuda or \
+            (dev is not None and t.device != dev) or (shape is not None and t.shape != shape):
+        _matrix(t, name, (dtype,), shape, dev)     # raises what is wrong
+    rows, cols = t.shape
+    ld, step = t.stride()
+    wide = -(-cols // unit) * unit
     if rows == 1:
-        ld = m16
-    if ld % 16 or ld < m16 or v.data_ptr() % 16 or not _room(v, (rows - 1) * ld + m16):
-        raise ValueError(f"{name} needs 16-byte aligned rows that are readable up to a multiple of 16 "
-                         "values, as quantize_fp8 returns them")
-    return rows, m, ld
-
-
-def _fp8_scales(s, name, shape, dev):
-    """Row stride of an 8-bit array's e8m0 scales, laid out likewise."""
-    rows, G, ld = _matrix(s, name, (E8M0,), shape, dev)
-    if rows == 1:
-        ld = _up(G, 4)
-    if ld % 4 or ld < _up(G, 4) or s.data_ptr() % 4 or not _room(s, (rows - 1) * ld + _up(G, 4)):
-        raise ValueError(f"{name} needs 4-byte aligned rows that are readable up to a multiple of 4 "
-                         "scales, as quantize_fp8 returns them")
-    return ld
+        ld = wide
+    if (step != 1 and cols > 1) or ld % unit or ld < wide or t.data_ptr() % unit or \
+            t.storage_offset() + (rows - 1) * ld + wide > t.untyped_storage().nbytes():
+        raise ValueError(f"{name} needs contiguous rows, aligned to {unit} bytes and readable up to a "
+                         f"multiple of {unit}, as quantize_fp8 returns them")
+    return rows, cols, ld
 
 
 def _result(n, T, tokens_first, dtype, dev):
@@ -712,10 +702,10 @@ def matmul_fp8(W8: torch.Tensor, w_scales: torch.Tensor, X8: torch.Tensor, x_sca
     X8 [T, m] and x_scales from :func:`quantize_fp8` or :func:`rmsnorm_fp8`.
     Returns [n, T] as :func:`dequant_matmul` does, or [T, n] with
     ``tokens_first``, in ``dtype`` (float32, float16 or bfloat16)."""
-    T, m, ldx = _fp8_values(X8, "X8")
+    T, m, ldx = _padded(X8, "X8", E4M3, 16)
     dev, G = X8.device, -(-m // FP8_BLOCK)
-    ldxs = _fp8_scales(x_scales, "x_scales", (T, G), dev)
-    n, mw, ldw = _fp8_values(W8, "W8", dev)
+    ldxs = _padded(x_scales, "x_scales", E8M0, 4, dev, (T, G))[2]
+    n, mw, ldw = _padded(W8, "W8", E4M3, 16, dev)
     if mw != m:
         raise ValueError(f"W8 has {mw} features and X8 {m}")
     rows = w_scales.shape[0] if w_scales.dim() == 2 else -1
@@ -723,15 +713,15 @@ def matmul_fp8(W8: torch.Tensor, w_scales: torch.Tensor, X8: torch.Tensor, x_sca
         raise ValueError(f"w_scales must have a row for each row or for each 128 rows of W8 (got {rows})")
     e8m0 = w_scales.dtype == E8M0
     if e8m0:
-        ldws = _fp8_scales(w_scales, "w_scales", (rows, G), dev)
+        ldws = _padded(w_scales, "w_scales", E8M0, 4, dev, (rows, G))[2]
     else:
         ldws = _matrix(w_scales, "w_scales", (torch.float32, E8M0), (rows, G), dev)[2]
     with _device(dev):
         Y = _result(n, T, tokens_first, dtype, dev)
-        _check(library().ojbkq_matmul_fp8(_ptr(W8), ldw, _ptr(w_scales), 1 if e8m0 else 0,
-                                          1 if rows == n else 128, ldws, n, m, _ptr(X8), ldx,
-                                          _ptr(x_scales), ldxs, T, _ptr(Y), FP8_TYPES[dtype],
-                                          1 if tokens_first else 0, Y.shape[1], _stream(dev)))
+        _check(library().ojbkq_matmul_fp8(_at(W8), ldw, _at(w_scales), 1 if e8m0 else 0,
+                                          1 if rows == n else 128, ldws, n, m, _at(X8), ldx,
+                                          _at(x_scales), ldxs, T, _at(Y), FP8_TYPES[dtype],
+                                          1 if tokens_first else 0, Y.shape[1], _raw_stream(dev)))
     return Y
 
 
@@ -748,11 +738,11 @@ def dequant_matmul_fp8(packed: torch.Tensor, scales: torch.Tensor, zeros: torch.
     ``workspace``: a uint8 device tensor of
     ``ojbkq_dequant_matmul_fp8_workspace_bytes`` bytes (allocated here when
     None and needed)."""
-    T, mx, ldx = _fp8_values(X8, "X8")
+    T, mx, ldx = _padded(X8, "X8", E4M3, 16)
     m, dev = int(m), X8.device
     if mx != m:
         raise ValueError(f"X8 has {mx} features, expected {m}")
-    ldxs = _fp8_scales(x_scales, "x_scales", (T, -(-m // FP8_BLOCK)), dev)
+    ldxs = _padded(x_scales, "x_scales", E8M0, 4, dev, (T, -(-m // FP8_BLOCK)))[2]
     n = packed.shape[0]
     _need(packed, "packed", torch.int32, (n, packed_words(m, bits)), dev)
     group = 0 if group >= m else int(group)
@@ -771,10 +761,10 @@ def dequant_matmul_fp8(packed: torch.Tensor, scales: torch.Tensor, zeros: torch.
             if not workspace.is_contiguous():
                 raise ValueError("workspace must be contiguous")
         Y = _result(n, T, tokens_first, dtype, dev)
-        _check(lib.ojbkq_dequant_matmul_fp8(_ptr(packed), _ptr(scales), _ptr(zeros), n, m,
-                                            int(bits), group, _ptr(X8), ldx, _ptr(x_scales),
-                                            ldxs, T, _ptr(Y), FP8_TYPES[dtype],
-                                            1 if tokens_first else 0, Y.shape[1], _ptr(workspace),
+        _check(lib.ojbkq_dequant_matmul_fp8(_at(packed), _at(scales), _at(zeros), n, m,
+                                            int(bits), group, _at(X8), ldx, _at(x_scales),
+                                            ldxs, T, _at(Y), FP8_TYPES[dtype],
+                                            1 if tokens_first else 0, Y.shape[1], _at(workspace),
                                             0 if workspace is None else workspace.numel(),
-                                            _stream(dev)))
+                                            _raw_stream(dev)))
     return Y

@@ -1,75 +1,144 @@
 // Products with 8-bit activations for few tokens: a decoding step, a small
 // batch, a narrow layer.
+#include "device.h"
 #include "fp8_product.h"
 
 namespace ojbkq {
 namespace {
 
+// 4 bytes per lane straight to LDS, lane i's at lds + 4 i (load_to_lds16_at's
+// narrow form).
+__device__ __forceinline__ void load_to_lds4_at(const void* src, const void* lds) {
+  const uint32_t a = __builtin_amdgcn_readfirstlane(lds_address(lds));
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "{m0}"(a) : "memory");
+}
+// All but the youngest N of the wave's loads have arrived.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N < 64, "six bits");
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
+
 // Y for few tokens.  Bound by reading the weights (for the fewest tokens by
 // latency), so a workgroup takes few channels, 16 RB, for all features, and its
-// eight waves split the features: chunks of 128 go round the waves, which meet
-// at the end in LDS, where their sums are added in wave order.  Lane l holds
-// features 32 (l / 16) .. + 31 of a chunk, of channel l % 16 and of token l %
-// 16, both brought to bf16 in registers (which holds an e4m3 value times its
-// power-of-two scale, and a code less its zero point, exactly): product s of
-// the chunk's four v_mfma_f32_16x16x32_bf16 takes its features 8 s .. + 7.
-// (The matrix cores' 8-bit products keep about 17 bits beside the largest of
-// eight neighbours; these keep float32's.)  The activations are the A operand,
-// so a lane's four sums belong to one channel and take its scale.
+// eight waves split the features: batches of up to four chunks of 128 go round
+// the waves, which meet at the end in LDS, where their sums are added in wave
+// order.  A lane's operands are 32 features of channel l % 16 and of token l %
+// 16, both brought to 16 bits in registers, a quarter of them to each of the
+// chunk's four products of 16 x 16 x 32.  (The matrix cores' 8-bit products
+// keep about 13 bits beside the largest of eight neighbours; these keep
+// float32's.)  The activations are the A operand, so a lane's four sums belong
+// to one channel and take its scale.
+//   e4m3 weights: both in bf16, which holds a value times a power of two.
+//   Codes: both in fp16, without the scales.  A code q set into the low bits of
+//   fp16's 1024 is 1024 + q, from which a packed subtraction takes 1024 + z:
+//   three operations to two codes, against six by way of float32 (14336 x 4096,
+//   24 tokens: 482 vector instructions a chunk of 32 channels and tokens).
+//
+// Read from memory that way, neighbouring lanes would be rows apart, and every
+// lane's 16 bytes an access of the cache by itself (690 accesses a chunk of 32
+// channels and tokens; they were the bound).  So a wave's rows come straight to
+// LDS, neighbouring lanes along a row, into a ring of kDepth chunks of its own;
+// no barrier is needed until the end.
 template <int SRC, int RB, int NB>
-__global__ __launch_bounds__(512) void product_few8_kernel(Product8Args a) {
-  constexpr int kTok = 16 * NB, kChan = 16 * RB, kRed = kChan * kTok;
-  constexpr int kDepth = RB * NB == 1 ? 4 : RB * NB <= 4 ? 2 : 1;   // chunks under way
-  __shared__ float red[8 * kRed];
+struct Few {
+  static constexpr int kTok = 16 * NB, kChan = 16 * RB, kWaves = 8;
+  static constexpr int kPitch = kChan + 4, kRed = kTok * kPitch;   // floats of a wave's sums, by tokens
+  static constexpr int kRow = SRC ? 16 * SRC : 128;                      // bytes of a chunk's row of weights
+  static constexpr int kW = (kChan * kRow + 1023) / 1024 * 1024, kX = kTok * 128, kStage = kW + kX;
+  static constexpr int kWide = kW / 1024, kLoads = kWide + kX / 1024;     // 16-byte loads of a chunk
+  static constexpr int kScales = RB * (SRC ? 2 : 1) + NB;                // 4-byte loads of a batch
+  static constexpr int kDepth = kWaves * (4 * kStage + 2 * kScales * 256) <= 160 * 1024 ? 4 : 2;
+  static constexpr int kRing = kWaves * kDepth * kStage, kSums = kWaves * kRed * 4;
+};
+
+template <int SRC, int RB, int NB>
+__global__ __launch_bounds__(512) void product_few8_kernel(Product8Args a, int batch) {
+  typedef Few<SRC, RB, NB> F;
+  constexpr int kTok = F::kTok, kChan = F::kChan, kWaves = F::kWaves, kDepth = F::kDepth;
+  __shared__ __align__(16) uint8_t lds[F::kRing > F::kSums ? F::kRing : F::kSums];
+  __shared__ uint32_t scales[kWaves][2][F::kScales][64];   // of two batches in turn
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i16 = lane & 15, g4 = lane >> 4;
   const int64_t J0 = (int64_t)blockIdx.x * kChan, T0 = (int64_t)blockIdx.y * kTok;
-  const int nch = (int)((a.m + 127) / 128);
+  const int nch = (int)((a.m + 127) >> 7);
+  uint8_t* const ring = lds + wave * (kDepth * F::kStage);
 
   // rows past the last one repeat it: they feed only sums that are not stored
-  int64_t j[RB], t[NB];
-#pragma unroll
-  for (int x = 0; x < RB; ++x) j[x] = J0 + 16 * x + i16 < a.n ? J0 + 16 * x + i16 : a.n - 1;
-#pragma unroll
-  for (int y = 0; y < NB; ++y) t[y] = T0 + 16 * y + i16 < a.T ? T0 + 16 * y + i16 : a.T - 1;
+  auto channel = [&](int r) { return J0 + r < a.n ? J0 + r : a.n - 1; };
+  auto token = [&](int r) { return T0 + r < a.T ? T0 + r : a.T - 1; };
+  const uint32_t* const P = a.P;
 
-  struct Stage {
-    uint32_t w[RB][SRC ? SRC : 8];   // 32 e4m3 values (SRC = 0) or codes of SRC bits
-    float s[RB], z[RB];
-    u4 x[NB][2];
-    uint32_t xs[NB];
+  // ---- memory to LDS --------------------------------------------------------
+  // A row of 128 bytes in LDS has its 16-byte piece p at place p ^ (row % 8),
+  // one of 64 bytes (4-bit codes) at p ^ (row / 4 % 4), which spreads the reads
+  // below over the banks; load h of a wave fills 1 KB, lane i its 16 bytes from
+  // 16 i on.
+  const int r8 = lane >> 3, p8 = (lane & 7) ^ r8;
+  // whole pieces behind the last feature are read from the row's first one
+  auto load_rows = [&](const uint8_t* row, int64_t k, uint8_t* to) {
+    load_to_lds16_at(row + k + (k + 16 * p8 < a.m ? 16 * p8 : 0), to);
   };
-  // 32 e4m3 values of a row from feature k on, in pieces of 16 (of which one
-  // with any feature below m is readable)
-  auto run = [&](const uint8_t* row, int64_t k, u4 (&v)[2]) {
+  const bool wide = SRC == 0 || (a.wpr % 4 == 0 && reinterpret_cast<uintptr_t>(P) % 16 == 0);
+  auto load_chunk = [&](int c, int slot) {
+    uint8_t* const w = ring + slot * F::kStage;
+    const int64_t k = 128 * (int64_t)c;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      v[h] = k + 16 * h < a.m ? *reinterpret_cast<const u4*>(row + k + 16 * h) : u4{0u, 0u, 0u, 0u};
+    for (int h = 0; h < F::kWide; ++h) {
+      if constexpr (SRC == 0) {
+        load_rows(a.W8 + channel(8 * h + r8) * a.ldw, k, w + 1024 * h);
+      } else if (wide && k + 128 <= a.m) {
+        constexpr int kPieces = kChan * SRC;
+        const int u = 64 * h + lane < kPieces ? 64 * h + lane : kPieces - 1;
+        const int r = u / SRC, p = SRC == 4 ? (u % SRC) ^ ((r >> 2) & 3) : u % SRC;
+        load_to_lds16_at(P + channel(r) * a.wpr + 4 * SRC * (int64_t)c + 4 * p, w + 1024 * h);
+      } else {
+        // word by word (words behind the row's last one: its activations are 0)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          constexpr int kWords = kChan * SRC * 4;
+          int u = 256 * h + 64 * e + lane;
+          u = u < kWords ? u : kWords - 1;
+          const int r = u / (4 * SRC), v = u % (4 * SRC);
+          const int64_t at = 4 * SRC * (int64_t)c + (SRC == 4 ? v ^ ((r & 12)) : v);
+          load_to_lds4_at(P + channel(r) * a.wpr + (at < a.wpr ? at : a.wpr - 1), w + 1024 * h + 256 * e);
+        }
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2 * NB; ++h) load_rows(a.X8 + token(8 * h + r8) * a.ldx, k, w + F::kW + 1024 * h);
   };
-  auto fetch = [&](int c, Stage& st) {
-    const int64_t k = 128 * (int64_t)c + 32 * g4;
+  // Scales of the four chunks from c0 on (a multiple of 4): float32 ones with a
+  // lane to each row and chunk, e8m0 ones with a lane to the four of a row.
+  auto load_scales = [&](int c0, uint32_t (*to)[64]) {
+    const int q = c0 + (lane & 3) < nch ? c0 + (lane & 3) : nch - 1;
+    const uint32_t b = a.ws_div == 1 ? (uint32_t)q : (uint32_t)q / a.ws_div;
 #pragma unroll
     for (int x = 0; x < RB; ++x) {
-      if constexpr (SRC == 0) {
-        u4 v[2];
-        run(a.W8 + j[x] * a.ldw, k, v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) st.w[x][e] = v[e >> 2][e & 3];
-      } else {
-        const uint32_t* p = a.P + j[x] * a.wpr;
-        const int64_t wi = k / 32 * SRC;
-#pragma unroll
-        for (int e = 0; e < SRC; ++e) st.w[x][e] = p[wi + e < a.wpr ? wi + e : a.wpr - 1];
-        st.z[x] = a.Z[j[x] * a.ws_ld + c / a.ws_div];
-      }
-      st.s[x] = weight_scale(a, j[x], c);
+      const uint8_t* const S = static_cast<const uint8_t*>(a.ws);
+      const int64_t j = channel(16 * x + (lane >> 2)) >> a.ws_shift, j8 = channel(16 * x + i16) >> a.ws_shift;
+      load_to_lds4_at(SRC == 0 && a.ws_e8m0 ? S + j8 * a.ws_ld + c0 : S + 4 * (j * a.ws_ld + b), to[x]);
+      if constexpr (SRC != 0) load_to_lds4_at(a.Z + j * a.ws_ld + b, to[RB + x]);
     }
 #pragma unroll
-    for (int y = 0; y < NB; ++y) {
-      run(a.X8 + t[y] * a.ldx, k, st.x[y]);
-      st.xs[y] = a.xs[t[y] * a.lds + c];
-    }
+    for (int y = 0; y < NB; ++y)
+      load_to_lds4_at(a.xs + token(16 * y + i16) * a.lds + c0, to[F::kScales - NB + y]);
+  };
+
+  // this wave's chunks, numbered: i is chunk i % batch of batch wave + 8 (i /
+  // batch); the last batch may be short
+  const int batches = (nch + batch - 1) / batch;
+  const int mine = wave < batches ? (batches - wave + kWaves - 1) / kWaves : 0;
+  const int shift = batch == 4 ? 2 : batch - 1;
+  auto chunk_of = [&](int i) { return ((wave + kWaves * (i >> shift)) << shift) + (i & (batch - 1)); };
+  int count = mine << shift;
+  if (mine && chunk_of(count - 1) >= nch) count -= chunk_of(count - 1) - (nch - 1);
+  auto load = [&](int i) {
+    const int c = chunk_of(i);
+    if ((i & (batch - 1)) == 0) load_scales(c & ~3, scales[wave][(i >> shift) & 1]);
+    load_chunk(c, i & (kDepth - 1));
   };
 
   v4 acc[RB][NB];
@@ -77,128 +146,223 @@ __global__ __launch_bounds__(512) void product_few8_kernel(Product8Args a) {
   for (int x = 0; x < RB; ++x)
 #pragma unroll
     for (int y = 0; y < NB; ++y) acc[x][y] = v4{0.f, 0.f, 0.f, 0.f};
-  auto products = [&](int c, Stage& st) {
-    const int64_t k = 128 * (int64_t)c + 32 * g4;
-    const bool whole = 128 * (int64_t)(c + 1) <= a.m;
-    if (!whole) {
-      // what stands behind a row's last value is not used
+
+#pragma unroll 1
+  for (int i = 0; i < kDepth && i < count; ++i) load(i);
+#pragma unroll 1
+  for (int i = 0; i < count; ++i) {
+    // chunk i has arrived when no more loads are under way than the chunks
+    // behind it have (at least kLoads each)
+    const int behind = count - 1 - i < kDepth - 1 ? count - 1 - i : kDepth - 1;
+    if (behind == 3) wait_loads<3 * F::kLoads>();
+    else if (behind == 2) wait_loads<2 * F::kLoads>();
+    else if (behind == 1) wait_loads<F::kLoads>();
+    else wait_loads<0>();
+
+    const int c = chunk_of(i), q = c & 3;
+    const uint8_t* const w = ring + (i & (kDepth - 1)) * F::kStage;
+    const uint32_t(*const sc)[64] = scales[wave][(i >> shift) & 1];
+    uint32_t cw[RB][SRC ? SRC : 8], cx[NB][8], cs[RB], cz[RB];
+    u4 cxs[NB];
+    // pieces g4 and 4 + g4 of a row of 128 bytes
+    auto row32 = [&](const uint8_t* rows, int r, uint32_t (&v)[8]) {
 #pragma unroll
-      for (int y = 0; y < NB; ++y)
+      for (int h = 0; h < 2; ++h) {
+        const u4 p = *reinterpret_cast<const u4*>(rows + 128 * r + 16 * ((4 * h + g4) ^ (r & 7)));
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          st.x[y][e >> 2][e & 3] = features_below(st.x[y][e >> 2][e & 3], k + 4 * e, a.m);
+        for (int e = 0; e < 4; ++e) v[4 * h + e] = p[e];
+      }
+    };
+#pragma unroll
+    for (int x = 0; x < RB; ++x) {
+      const int r = 16 * x + i16;
       if constexpr (SRC == 0) {
+        row32(w, r, cw[x]);
+        cs[x] = a.ws_e8m0 ? sc[x][i16] : sc[x][4 * i16 + q];
+      } else {
+        // pieces and features as the activations': 16 codes from each of two
+        // places, SRC half words; word e takes half word e of both
+        const uint8_t* const at = w + F::kRow * r;
+        if constexpr (SRC == 4) {
+          u2v h[2];
 #pragma unroll
-        for (int x = 0; x < RB; ++x)
+          for (int f = 0; f < 2; ++f)
+            h[f] = *reinterpret_cast<const u2v*>(at + 16 * ((2 * f + (g4 >> 1)) ^ ((r >> 2) & 3)) + 8 * (g4 & 1));
 #pragma unroll
-          for (int e = 0; e < 8; ++e) st.w[x][e] = features_below(st.w[x][e], k + 4 * e, a.m);
+          for (int e = 0; e < 4; ++e)
+            cw[x][e] = __builtin_amdgcn_perm(h[1][e >> 1], h[0][e >> 1], (e & 1) ? 0x07060302u : 0x05040100u);
+        } else {
+          const uint16_t* const h = reinterpret_cast<const uint16_t*>(at) + SRC * g4;
+#pragma unroll
+          for (int e = 0; e < SRC; ++e) cw[x][e] = h[e] | ((uint32_t)h[4 * SRC + e] << 16);
+        }
+        cs[x] = sc[x][4 * i16 + q];
+        cz[x] = sc[RB + x][4 * i16 + q];
       }
     }
+#pragma unroll
+    for (int y = 0; y < NB; ++y) {
+      row32(w + F::kW, 16 * y + i16, cx[y]);
+      // (the scales of four chunks) of this lane's token, or of its four sums'
+      const uint32_t* const of = sc[F::kScales - NB + y];
+      if constexpr (SRC == 0) cxs[y][0] = of[i16];
+      else cxs[y] = *reinterpret_cast<const u4*>(of + 4 * g4);
+    }
+    wait_lds();
+    if (i + kDepth < count) load(i + kDepth);
+
+    if (128 * (int64_t)(c + 1) > a.m) {
+      // what stands behind a row's last value is not used
+      const int64_t k = 128 * (int64_t)c + 16 * g4;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int64_t ke = k + 64 * (e >> 2) + 4 * (e & 3);
+#pragma unroll
+        for (int y = 0; y < NB; ++y) cx[y][e] = features_below(cx[y][e], ke, a.m);
+        if constexpr (SRC == 0)
+#pragma unroll
+          for (int x = 0; x < RB; ++x) cw[x][e] = features_below(cw[x][e], ke, a.m);
+      }
+    }
+
     v4 d[RB][NB];
 #pragma unroll
     for (int x = 0; x < RB; ++x)
 #pragma unroll
       for (int y = 0; y < NB; ++y) d[x][y] = v4{0.f, 0.f, 0.f, 0.f};
-    float power[RB];
+    auto xscale = [&](int y, int r) { return from_e8m0((cxs[y][r] >> (8 * q)) & 0xffu); };
     if constexpr (SRC == 0) {
+      SplitScale s[RB];
 #pragma unroll
-      for (int x = 0; x < RB; ++x) {
-        const SplitScale sp = split_scale(st.s[x]);
-        power[x] = sp.power;
-        st.s[x] = sp.rest;
-      }
-    }
+      for (int x = 0; x < RB; ++x)
+        s[x] = split_scale(a.ws_e8m0 ? from_e8m0((cs[x] >> (8 * q)) & 0xffu) : __uint_as_float(cs[x]));
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      b8 fx[NB];
+      for (int p = 0; p < 4; ++p) {
+        b8 fx[NB];
 #pragma unroll
-      for (int y = 0; y < NB; ++y)
-        fx[y] = to_bf16(st.x[y][s >> 1][2 * (s & 1)], st.x[y][s >> 1][2 * (s & 1) + 1],
-                        from_e8m0(st.xs[y]));
+        for (int y = 0; y < NB; ++y) fx[y] = to_bf16(cx[y][2 * p], cx[y][2 * p + 1], xscale(y, 0));
 #pragma unroll
-      for (int x = 0; x < RB; ++x) {
-        b8 fw;
-        if constexpr (SRC == 0) {
-          fw = to_bf16(st.w[x][2 * s], st.w[x][2 * s + 1], power[x]);
-        } else {
-          // (codes past the last one are zero bits; their activations are 0)
-          const float z = whole_zero<SRC>(st.z[x]);
+        for (int x = 0; x < RB; ++x) {
+          const b8 fw = to_bf16(cw[x][2 * p], cw[x][2 * p + 1], s[x].power);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) fw[e] = (__bf16)((float)code_of<SRC>(st.w[x], 8 * s + e) - z);
+          for (int y = 0; y < NB; ++y)
+            d[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[y], fw, d[x][y], 0, 0, 0);
         }
+      }
+#pragma unroll
+      for (int x = 0; x < RB; ++x)
 #pragma unroll
         for (int y = 0; y < NB; ++y)
-          d[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[y], fw, d[x][y], 0, 0, 0);
-      }
-    }
 #pragma unroll
-    for (int x = 0; x < RB; ++x)
+          for (int r = 0; r < 4; ++r)
+            acc[x][y][r] = __builtin_fmaf(d[x][y][r], s[x].rest, acc[x][y][r]);
+    } else {
+      h2 less[RB];   // 1024 + z
+#pragma unroll
+      for (int x = 0; x < RB; ++x) {
+        const _Float16 z = (_Float16)(1024.f + whole_zero<SRC>(__uint_as_float(cz[x])));
+        less[x] = h2{z, z};
+      }
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        // features 4 p .. + 3 of both halves, in turn
+        h8 fx[NB];
+#pragma unroll
+        for (int y = 0; y < NB; ++y) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t v = __builtin_amdgcn_perm(cx[y][4 + p], cx[y][p], h ? 0x07030602u : 0x05010400u);
+            const h2 lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 1.f, false);
+            const h2 hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 1.f, true);
+            fx[y][4 * h] = lo.x;
+            fx[y][4 * h + 1] = lo.y;
+            fx[y][4 * h + 2] = hi.x;
+            fx[y][4 * h + 3] = hi.y;
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < RB; ++x) {
+          h8 fw;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            constexpr uint32_t kMask = 0x00010001u * ((1u << SRC) - 1u);
+            const int b = (4 * p + e) * SRC, at = b >> 4, sh = b & 15;
+            uint32_t v = (cw[x][at] >> sh) & kMask;
+            if (sh + SRC > 16)   // a code that goes on in the next half word
+              v = ((cw[x][at] >> sh) & (0x00010001u * ((1u << (16 - sh)) - 1u))) |
+                  ((cw[x][at + 1 < SRC ? at + 1 : at] << (16 - sh)) & kMask &
+                   ~(0x00010001u * ((1u << (16 - sh)) - 1u)));
+            const h2 f = __builtin_bit_cast(h2, v | 0x64006400u) - less[x];
+            fw[2 * e] = f.x;
+            fw[2 * e + 1] = f.y;
+          }
+#pragma unroll
+          for (int y = 0; y < NB; ++y)
+            d[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fx[y], fw, d[x][y], 0, 0, 0);
+        }
+      }
 #pragma unroll
       for (int y = 0; y < NB; ++y)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) acc[x][y][r] = __builtin_fmaf(d[x][y][r], st.s[x], acc[x][y][r]);
-  };
-
-  Stage st[kDepth];
+        for (int r = 0; r < 4; ++r) {
+          const float sx = xscale(y, r);
 #pragma unroll
-  for (int d = 0; d < kDepth; ++d)
-    if (wave + 8 * d < nch) fetch(wave + 8 * d, st[d]);
-  for (int c = wave; c < nch; c += 8 * kDepth) {
-#pragma unroll
-    for (int d = 0; d < kDepth; ++d) {
-      const int cd = c + 8 * d;
-      if (cd >= nch) break;
-      Stage cur = st[d];
-      if (cd + 8 * kDepth < nch) fetch(cd + 8 * kDepth, st[d]);
-      products(cd, cur);
+          for (int x = 0; x < RB; ++x)
+            acc[x][y][r] = __builtin_fmaf(d[x][y][r] * sx, __uint_as_float(cs[x]), acc[x][y][r]);
+        }
     }
   }
 
   // the waves' sums, in wave order: lane l holds tokens 4 (l / 16) + r of
   // channel l % 16
+  __syncthreads();
+  float* const red = reinterpret_cast<float*>(lds);
 #pragma unroll
   for (int x = 0; x < RB; ++x)
 #pragma unroll
     for (int y = 0; y < NB; ++y)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        red[wave * kRed + (16 * x + i16) * kTok + 16 * y + 4 * g4 + r] = acc[x][y][r];
+        red[wave * F::kRed + (16 * y + 4 * g4 + r) * F::kPitch + 16 * x + i16] = acc[x][y][r];
   __syncthreads();
-  for (int e = tid; e < kRed; e += 512) {
+  for (int e = tid; e < kChan * kTok; e += 64 * kWaves) {
     const int jj = a.tokens_first ? e % kChan : e / kTok, tt = a.tokens_first ? e / kChan : e % kTok;
-    float v = red[jj * kTok + tt];
+    float v = red[tt * F::kPitch + jj];
 #pragma unroll
-    for (int w = 1; w < 8; ++w) v += red[w * kRed + jj * kTok + tt];
+    for (int w = 1; w < kWaves; ++w) v += red[w * F::kRed + tt * F::kPitch + jj];
     if (J0 + jj < a.n && T0 + tt < a.T) store_y(a, J0 + jj, T0 + tt, v);
   }
 }
 
 template <int SRC, int NB>
 hipError_t launch_rb(const Product8Args& a, hipStream_t s) {
-  // as many channels per workgroup as leave one for every CU
-  const int64_t gy = (a.T + 16 * NB - 1) / (16 * NB);
+  const int64_t gy = (a.T + 16 * NB - 1) / (16 * NB), nch = (a.m + 127) / 128;
+  // four chunks to a batch where that gives every wave one
+  const int batch = nch >= 32 ? 4 : nch >= 16 ? 2 : 1;
   auto grid = [&](int rb) { return dim3((unsigned)((a.n + 16 * rb - 1) / (16 * rb)), (unsigned)gy); };
-  if ((a.n + 63) / 64 * gy >= 256)
-    product_few8_kernel<SRC, 4, NB><<<grid(4), dim3(512), 0, s>>>(a);
-  else if ((a.n + 31) / 32 * gy >= 256)
-    product_few8_kernel<SRC, 2, NB><<<grid(2), dim3(512), 0, s>>>(a);
+  // 32 or, of codes, 64 channels per workgroup where that leaves one for every CU
+  if constexpr (SRC != 0 && NB == 1)
+    if ((a.n + 63) / 64 * gy >= 256) {
+      product_few8_kernel<SRC, 4, NB><<<grid(4), dim3(512), 0, s>>>(a, batch);
+      return hipGetLastError();
+    }
+  if ((a.n + 31) / 32 * gy >= 256)
+    product_few8_kernel<SRC, 2, NB><<<grid(2), dim3(512), 0, s>>>(a, batch);
   else
-    product_few8_kernel<SRC, 1, NB><<<grid(1), dim3(512), 0, s>>>(a);
+    product_few8_kernel<SRC, 1, NB><<<grid(1), dim3(512), 0, s>>>(a, batch);
   return hipGetLastError();
 }
 
 template <int SRC>
 hipError_t launch(const Product8Args& a, hipStream_t s) {
-  if (a.T <= 16) return launch_rb<SRC, 1>(a, s);
-  if (a.T <= 32) return launch_rb<SRC, 2>(a, s);
-  return launch_rb<SRC, 4>(a, s);
+  return a.T <= 16 ? launch_rb<SRC, 1>(a, s) : launch_rb<SRC, 2>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_product_few8(const Product8Args& a, int bits, hipStream_t stream) {
   // (the second dimension of a grid holds 65535)
-  const int64_t step = (int64_t)65535 * 64;
+  const int64_t step = (int64_t)65535 * 32;
   for (int64_t t = 0; t < a.T; t += step) {
     Product8Args b = a;
     const size_t size = a.ytype == 0 ? 4 : 2;

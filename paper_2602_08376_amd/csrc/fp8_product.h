@@ -8,19 +8,16 @@ namespace ojbkq {
 
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef float v4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2v __attribute__((ext_vector_type(2)));
 
 // 2^(code - 127) (code 0: 2^-127, the one below float32's normal range).
 __device__ __forceinline__ float from_e8m0(uint32_t code) {
-  return __uint_as_float(code ? code << 23 : 1u << 22);
-}
-
-// Scale of row j, block b of 128 features of the weights.
-__device__ __forceinline__ float weight_scale(const Product8Args& a, int64_t j, uint32_t b) {
-  const int64_t at = (j >> a.ws_shift) * a.ws_ld + b / a.ws_div;
-  return a.ws_e8m0 ? from_e8m0(static_cast<const uint8_t*>(a.ws)[at])
-                   : static_cast<const float*>(a.ws)[at];
+  const uint32_t b = code << 23;
+  return __uint_as_float(b > (1u << 22) ? b : 1u << 22);
 }
 
 // A weight scale as a power of two, which goes to the weights in bf16 or in the
