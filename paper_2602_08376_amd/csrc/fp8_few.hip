@@ -22,9 +22,8 @@ __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)"
 
 // Y for few tokens.  Bound by reading the weights (for the fewest tokens by
 // latency), so a workgroup takes few channels, 16 RB, for all features, and its
-// eight waves split the features: batches of up to four chunks of 128 go round
-// the waves, which meet at the end in LDS, where their sums are added in wave
-// order.  A lane's operands are 32 features of channel l % 16 and of token l %
+// eight waves split the features: chunks of 128 go round the waves, which meet
+// at the end in LDS, where their sums are added in wave order.  A lane's operands are 32 features of channel l % 16 and of token l %
 // 16, both brought to 16 bits in registers, a quarter of them to each of the
 // chunk's four products of 16 x 16 x 32.  (The matrix cores' 8-bit products
 // keep about 13 bits beside the largest of eight neighbours; these keep
@@ -46,19 +45,21 @@ struct Few {
   static constexpr int kTok = 16 * NB, kChan = 16 * RB, kWaves = 8;
   static constexpr int kPitch = kChan + 4, kRed = kTok * kPitch;   // floats of a wave's sums, by tokens
   static constexpr int kRow = SRC ? 16 * SRC : 128;                      // bytes of a chunk's row of weights
-  static constexpr int kW = (kChan * kRow + 1023) / 1024 * 1024, kX = kTok * 128, kStage = kW + kX;
-  static constexpr int kWide = kW / 1024, kLoads = kWide + kX / 1024;     // 16-byte loads of a chunk
-  static constexpr int kScales = RB * (SRC ? 2 : 1) + NB;                // 4-byte loads of a batch
-  static constexpr int kDepth = kWaves * (4 * kStage + 2 * kScales * 256) <= 160 * 1024 ? 4 : 2;
+  static constexpr int kW = (kChan * kRow + 1023) / 1024 * 1024, kX = kTok * 128;
+  // then a word for every channel and token with its scale, and of codes one
+  // with the zero point; lane i's from 4 i on
+  static constexpr int kS = kW + kX, kXs = kS + 256, kZ = kXs + 256, kStage = SRC ? kZ + 256 : kZ;
+  static constexpr int kDepth = kWaves * 4 * kStage <= 160 * 1024 ? 4 : 2;
+  static constexpr int kWide = kW / 1024;
+  static constexpr int kLoads = kWide + kX / 1024 + (kStage - kS) / 256;   // of a chunk, at least
   static constexpr int kRing = kWaves * kDepth * kStage, kSums = kWaves * kRed * 4;
 };
 
 template <int SRC, int RB, int NB>
-__global__ __launch_bounds__(512) void product_few8_kernel(Product8Args a, int batch) {
+__global__ __launch_bounds__(512) void product_few8_kernel(Product8Args a) {
   typedef Few<SRC, RB, NB> F;
   constexpr int kTok = F::kTok, kChan = F::kChan, kWaves = F::kWaves, kDepth = F::kDepth;
   __shared__ __align__(16) uint8_t lds[F::kRing > F::kSums ? F::kRing : F::kSums];
-  __shared__ uint32_t scales[kWaves][2][F::kScales][64];   // of two batches in turn
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i16 = lane & 15, g4 = lane >> 4;
@@ -110,36 +111,21 @@ __global__ __launch_bounds__(512) void product_few8_kernel(Product8Args a, int b
 #pragma unroll
     for (int h = 0; h < 2 * NB; ++h) load_rows(a.X8 + token(8 * h + r8) * a.ldx, k, w + F::kW + 1024 * h);
   };
-  // Scales of the four chunks from c0 on (a multiple of 4): float32 ones with a
-  // lane to each row and chunk, e8m0 ones with a lane to the four of a row.
-  auto load_scales = [&](int c0, uint32_t (*to)[64]) {
-    const int q = c0 + (lane & 3) < nch ? c0 + (lane & 3) : nch - 1;
-    const uint32_t b = a.ws_div == 1 ? (uint32_t)q : (uint32_t)q / a.ws_div;
-#pragma unroll
-    for (int x = 0; x < RB; ++x) {
-      const uint8_t* const S = static_cast<const uint8_t*>(a.ws);
-      const int64_t j = channel(16 * x + (lane >> 2)) >> a.ws_shift, j8 = channel(16 * x + i16) >> a.ws_shift;
-      load_to_lds4_at(SRC == 0 && a.ws_e8m0 ? S + j8 * a.ws_ld + c0 : S + 4 * (j * a.ws_ld + b), to[x]);
-      if constexpr (SRC != 0) load_to_lds4_at(a.Z + j * a.ws_ld + b, to[RB + x]);
-    }
-#pragma unroll
-    for (int y = 0; y < NB; ++y)
-      load_to_lds4_at(a.xs + token(16 * y + i16) * a.lds + c0, to[F::kScales - NB + y]);
-  };
-
-  // this wave's chunks, numbered: i is chunk i % batch of batch wave + 8 (i /
-  // batch); the last batch may be short
-  const int batches = (nch + batch - 1) / batch;
-  const int mine = wave < batches ? (batches - wave + kWaves - 1) / kWaves : 0;
-  const int shift = batch == 4 ? 2 : batch - 1;
-  auto chunk_of = [&](int i) { return ((wave + kWaves * (i >> shift)) << shift) + (i & (batch - 1)); };
-  int count = mine << shift;
-  if (mine && chunk_of(count - 1) >= nch) count -= chunk_of(count - 1) - (nch - 1);
+  // scales: a lane to each row (of the e8m0 ones a word, that of four chunks)
+  const bool bytes = SRC == 0 && a.ws_e8m0;
+  const int64_t srow = (channel(lane & (kChan - 1)) >> a.ws_shift) * a.ws_ld;
+  const uint8_t* const s_at = static_cast<const uint8_t*>(a.ws) + (bytes ? srow : 4 * srow);
+  const uint8_t* const xs_at = a.xs + token(lane & (kTok - 1)) * a.lds;
   auto load = [&](int i) {
-    const int c = chunk_of(i);
-    if ((i & (batch - 1)) == 0) load_scales(c & ~3, scales[wave][(i >> shift) & 1]);
+    const int c = wave + kWaves * i, c0 = c & ~3;
+    uint8_t* const to = ring + (i & (kDepth - 1)) * F::kStage;
+    const uint32_t b = a.ws_div == 1 ? (uint32_t)c : (uint32_t)c / a.ws_div;
+    load_to_lds4_at(s_at + (bytes ? (uint32_t)c0 : 4 * b), to + F::kS);
+    if constexpr (SRC != 0) load_to_lds4_at(a.Z + srow + b, to + F::kZ);
+    load_to_lds4_at(xs_at + c0, to + F::kXs);
     load_chunk(c, i & (kDepth - 1));
   };
+  const int count = wave < nch ? (nch - wave + kWaves - 1) / kWaves : 0;   // this wave's chunks
 
   v4 acc[RB][NB];
 #pragma unroll
@@ -159,9 +145,9 @@ __global__ __launch_bounds__(512) void product_few8_kernel(Product8Args a, int b
     else if (behind == 1) wait_loads<F::kLoads>();
     else wait_loads<0>();
 
-    const int c = chunk_of(i), q = c & 3;
+    const int c = wave + kWaves * i, q = c & 3;
     const uint8_t* const w = ring + (i & (kDepth - 1)) * F::kStage;
-    const uint32_t(*const sc)[64] = scales[wave][(i >> shift) & 1];
+    auto word = [&](int at, int n) { return *reinterpret_cast<const uint32_t*>(w + at + 4 * n); };
     uint32_t cw[RB][SRC ? SRC : 8], cx[NB][8], cs[RB], cz[RB];
     u4 cxs[NB];
     // pieces g4 and 4 + g4 of a row of 128 bytes
@@ -178,7 +164,6 @@ __global__ __launch_bounds__(512) void product_few8_kernel(Product8Args a, int b
       const int r = 16 * x + i16;
       if constexpr (SRC == 0) {
         row32(w, r, cw[x]);
-        cs[x] = a.ws_e8m0 ? sc[x][i16] : sc[x][4 * i16 + q];
       } else {
         // pieces and features as the activations': 16 codes from each of two
         // places, SRC half words; word e takes half word e of both
@@ -196,17 +181,16 @@ __global__ __launch_bounds__(512) void product_few8_kernel(Product8Args a, int b
 #pragma unroll
           for (int e = 0; e < SRC; ++e) cw[x][e] = h[e] | ((uint32_t)h[4 * SRC + e] << 16);
         }
-        cs[x] = sc[x][4 * i16 + q];
-        cz[x] = sc[RB + x][4 * i16 + q];
+        cz[x] = word(F::kZ, r);
       }
+      cs[x] = word(F::kS, r);
     }
 #pragma unroll
     for (int y = 0; y < NB; ++y) {
       row32(w + F::kW, 16 * y + i16, cx[y]);
       // (the scales of four chunks) of this lane's token, or of its four sums'
-      const uint32_t* const of = sc[F::kScales - NB + y];
-      if constexpr (SRC == 0) cxs[y][0] = of[i16];
-      else cxs[y] = *reinterpret_cast<const u4*>(of + 4 * g4);
+      if constexpr (SRC == 0) cxs[y][0] = word(F::kXs, 16 * y + i16);
+      else cxs[y] = *reinterpret_cast<const u4*>(w + F::kXs + 4 * (16 * y + 4 * g4));
     }
     wait_lds();
     if (i + kDepth < count) load(i + kDepth);
@@ -235,7 +219,7 @@ __global__ __launch_bounds__(512) void product_few8_kernel(Product8Args a, int b
       SplitScale s[RB];
 #pragma unroll
       for (int x = 0; x < RB; ++x)
-        s[x] = split_scale(a.ws_e8m0 ? from_e8m0((cs[x] >> (8 * q)) & 0xffu) : __uint_as_float(cs[x]));
+        s[x] = split_scale(bytes ? from_e8m0((cs[x] >> (8 * q)) & 0xffu) : __uint_as_float(cs[x]));
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
         b8 fx[NB];
@@ -336,20 +320,22 @@ __global__ __launch_bounds__(512) void product_few8_kernel(Product8Args a, int b
 
 template <int SRC, int NB>
 hipError_t launch_rb(const Product8Args& a, hipStream_t s) {
-  const int64_t gy = (a.T + 16 * NB - 1) / (16 * NB), nch = (a.m + 127) / 128;
-  // four chunks to a batch where that gives every wave one
-  const int batch = nch >= 32 ? 4 : nch >= 16 ? 2 : 1;
+  const int64_t gy = (a.T + 16 * NB - 1) / (16 * NB);
   auto grid = [&](int rb) { return dim3((unsigned)((a.n + 16 * rb - 1) / (16 * rb)), (unsigned)gy); };
-  // 32 or, of codes, 64 channels per workgroup where that leaves one for every CU
-  if constexpr (SRC != 0 && NB == 1)
-    if ((a.n + 63) / 64 * gy >= 256) {
-      product_few8_kernel<SRC, 4, NB><<<grid(4), dim3(512), 0, s>>>(a, batch);
+  // As many channels as leave work for 160 of the 256 CUs: fewer bring a second
+  // round of workgroups, each of which reads the activations again (us for 64 /
+  // 32 / 16 channels: codes 14336 x 4096, 24 tokens 16.5 / 19.1 / 27.4, 11008 x
+  // 4096 16.1 / 19.1 / 21.5; for 32 / 16: codes 4096 x 11008, 32 tokens, 128
+  // and 256 workgroups, 20.3 / 15.9).  64 e4m3 channels do not fit in LDS twice.
+  if constexpr (SRC != 0)
+    if ((a.n + 63) / 64 * gy >= 160) {
+      product_few8_kernel<SRC, 4, NB><<<grid(4), dim3(512), 0, s>>>(a);
       return hipGetLastError();
     }
-  if ((a.n + 31) / 32 * gy >= 256)
-    product_few8_kernel<SRC, 2, NB><<<grid(2), dim3(512), 0, s>>>(a, batch);
+  if ((a.n + 31) / 32 * gy >= 160)
+    product_few8_kernel<SRC, 2, NB><<<grid(2), dim3(512), 0, s>>>(a);
   else
-    product_few8_kernel<SRC, 1, NB><<<grid(1), dim3(512), 0, s>>>(a, batch);
+    product_few8_kernel<SRC, 1, NB><<<grid(1), dim3(512), 0, s>>>(a);
   return hipGetLastError();
 }
 
