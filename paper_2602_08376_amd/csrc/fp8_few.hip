@@ -1,17 +1,10 @@
 // Products with 8-bit activations for few tokens: a decoding step, a small
 // batch, a narrow layer.
-#include "device.h"
 #include "fp8_product.h"
 
 namespace ojbkq {
 namespace {
 
-// 4 bytes per lane straight to LDS, lane i's at lds + 4 i (load_to_lds16_at's
-// narrow form).
-__device__ __forceinline__ void load_to_lds4_at(const void* src, const void* lds) {
-  const uint32_t a = __builtin_amdgcn_readfirstlane(lds_address(lds));
-  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "{m0}"(a) : "memory");
-}
 // All but the youngest N of the wave's loads have arrived.
 template <int N>
 __device__ __forceinline__ void wait_loads() {

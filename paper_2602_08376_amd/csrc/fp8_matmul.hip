@@ -3,7 +3,6 @@
 //
 //   expand_codes_kernel  packed codes -> e4m3 values q - z, once
 //   product8_kernel      Y of e4m3 weights and activations, in tiles
-#include "device.h"
 #include "fp8_product.h"
 #include "kernels.h"
 
@@ -62,6 +61,11 @@ __device__ __forceinline__ void tile_of(int64_t tiles_n, int64_t& tj, int64_t& t
   tt = r / rows;
 }
 
+// Sums are formed where they stand (the compiler moves them, with the products
+// they come from, behind the branches and barriers that follow, and has to hold
+// all operands until then).
+__device__ __forceinline__ void pin(v4& v) { asm volatile("" : "+v"(v)); }
+
 template <class E, int N>
 __device__ __forceinline__ void store_run(E* p, const float (&v)[N], int64_t left) {
   typedef E Any __attribute__((ext_vector_type(N), aligned(sizeof(E))));
@@ -94,8 +98,9 @@ template <int NX, bool EXACT>
 __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, int64_t tiles_n) {
   constexpr int kTile = 32 * NX;
   __shared__ __align__(16) uint8_t sX[2][kTile * 128], sW[2][kTile * 128];
-  __shared__ uint32_t sxs[2][kTile];      // scales of a line for four stages
-  __shared__ float sws[2][4][kTile];
+  // scales of four stages: of a line of activations (a byte each), of a channel
+  // of weights (a float32 each, or e8m0 bytes in the first)
+  __shared__ __align__(16) uint32_t sxs[2][kTile], sws[2][4][kTile];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i16 = lane & 15, g4 = lane >> 4;
@@ -111,34 +116,37 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
   };
   auto channel_of = [](int line) { return (line & ~63) + 4 * (line & 15) + ((line >> 4) & 3); };
 
-  // load q of a wave fills lines 8 (4 wave + q) .. + 7; rows past the last one
-  // repeat it (they feed only results that are not stored)
-  uint32_t xoff[4], woff[4];
-  const int chunk = (lane & 7) ^ (lane >> 3);
+  // ---- memory to LDS --------------------------------------------------------
+  // Load q of a wave fills lines 8 (4 wave + q) .. + 7; rows past the last one
+  // repeat it (they feed only results that are not stored).  The four rows of a
+  // lane, each below 256, share a register.
+  uint32_t xrows = 0, wrows = 0;
+  const int last_t = (int)(a.T - 1 - T0 < kTile - 1 ? a.T - 1 - T0 : kTile - 1);
+  const int last_j = (int)(a.n - 1 - J0 < kTile - 1 ? a.n - 1 - J0 : kTile - 1);
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const int line = 8 * (4 * wave + q) + (lane >> 3);
-    const int64_t t = T0 + token_of(line), j = J0 + channel_of(line);
-    xoff[q] = (uint32_t)((t < a.T ? t : a.T - 1) - T0) * (uint32_t)a.ldx + 16 * chunk;
-    woff[q] = (uint32_t)((j < a.n ? j : a.n - 1) - J0) * (uint32_t)a.ldw + 16 * chunk;
+    const int t = token_of(line), j = channel_of(line);
+    xrows |= (uint32_t)(t < last_t ? t : last_t) << (8 * q);
+    wrows |= (uint32_t)(j < last_j ? j : last_j) << (8 * q);
   }
   const uint8_t* const xbase = a.X8 + T0 * a.ldx;
   const uint8_t* const wbase = a.W8 + J0 * a.ldw;
-  auto load = [&](int st, int buf) {
+  const uint32_t piece = 16 * ((lane & 7) ^ (lane >> 3));
+  // (a piece past the last feature reads the row's first one; mask_tail clears it)
+  auto load = [&](const uint8_t* base, uint32_t rows, uint32_t ld, int st, uint8_t* to) {
     const int64_t k0 = 128 * (int64_t)st;
-    // a chunk past the last feature reads the row's first one; mask_tail
-    // clears it
-    const uint32_t back = k0 + 16 * chunk < a.m ? 0u : 16u * chunk;
+    const uint32_t at = k0 + piece < a.m ? piece : 0u;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      load_to_lds16(xbase + k0, xoff[q] - back, sX[buf] + 1024 * (4 * wave + q));
-      load_to_lds16(wbase + k0, woff[q] - back, sW[buf] + 1024 * (4 * wave + q));
-    }
+    for (int q = 0; q < 4; ++q)
+      load_to_lds16(base + k0, __builtin_amdgcn_ubfe(rows, 8 * q, 8) * ld + at, to + 1024 * (4 * wave + q));
   };
+  auto load_x = [&](int st) { load(xbase, xrows, (uint32_t)a.ldx, st, sX[st & 1]); };
+  auto load_w = [&](int st) { load(wbase, wrows, (uint32_t)a.ldw, st, sW[st & 1]); };
   // the last stage of a ragged row: everything from feature m on cleared
-  auto mask_tail = [&](int st, int buf) {
+  auto mask_tail = [&](int st) {
     const int left = (int)(a.m - 128 * (int64_t)st);
-    uint8_t* const line = (tid < kTile ? sX[buf] : sW[buf]) + 128 * (tid & (kTile - 1));
+    uint8_t* const line = (tid < kTile ? sX[st & 1] : sW[st & 1]) + 128 * (tid & (kTile - 1));
     for (int c = left / 16; c < 8; ++c) {
       u4* const p = reinterpret_cast<u4*>(line + 16 * (c ^ (tid & 7)));
       u4 v = *p;
@@ -147,38 +155,57 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
       *p = v;
     }
   };
-
-  // scales of four stages, a thread to a line of either operand: read at the
-  // first of the four before, in LDS at the last of them
-  const int sline = tid & (kTile - 1);
-  const int64_t srow = tid < kTile ? T0 + token_of(sline) : J0 + channel_of(sline);
-  const bool bytes = tid < kTile || a.ws_e8m0;   // (the same for a whole wave)
-  const uint8_t* const srow_at =
-      tid < kTile ? a.xs + (srow < a.T ? srow : a.T - 1) * a.lds
-                  : static_cast<const uint8_t*>(a.ws) +
-                        ((srow < a.n ? srow : a.n - 1) >> a.ws_shift) * a.ws_ld * (a.ws_e8m0 ? 1 : 4);
-  uint32_t sc[4] = {0u, 0u, 0u, 0u};
-  auto fetch_scales = [&](int quad) {
-    if (bytes) {
-      sc[0] = *reinterpret_cast<const uint32_t*>(srow_at + 4 * quad);
+  // a wave to 64 lines or channels (their addresses formed anew every time, not
+  // held in registers)
+  const bool bytes = a.ws_e8m0 != 0;
+  auto load_scales = [&](int quad) {
+    int w = wave;
+    __asm__("" : "+s"(w));
+    const int buf = quad & 1;
+    if (w < kTile / 64) {
+      const int t = token_of(64 * w + lane);
+      load_to_lds4_at(a.xs + (T0 + (t < last_t ? t : last_t)) * a.lds + 4 * quad, &sxs[buf][64 * w]);
     } else {
+      const int c0 = 64 * (w - kTile / 64), j = c0 + lane;
+      const int64_t at = ((J0 + (j < last_j ? j : last_j)) >> a.ws_shift) * a.ws_ld;
+      const uint8_t* const S = static_cast<const uint8_t*>(a.ws);
+      if (bytes) {
+        load_to_lds4_at(S + at + 4 * quad, &sws[buf][0][c0]);
+      } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t b = (uint32_t)(4 * quad + e < nst ? 4 * quad + e : nst - 1);
-        sc[e] = reinterpret_cast<const uint32_t*>(srow_at)[b / a.ws_div];
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t b = (uint32_t)(4 * quad + e < nst ? 4 * quad + e : nst - 1);
+          load_to_lds4_at(S + 4 * (at + (a.ws_div == 1 ? b : b / a.ws_div)), &sws[buf][e][c0]);
+        }
       }
     }
   };
-  auto put_scales = [&](int buf) {
-    if (tid < kTile) {
-      sxs[buf][sline] = sc[0];
-    } else if (bytes) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sws[buf][e][sline] = from_e8m0((sc[0] >> (8 * e)) & 0xffu);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sws[buf][e][sline] = __uint_as_float(sc[e]);
+  const bool ragged = (a.m & 127) != 0;
+  auto arrived = [&](int st) {   // stage st, of which every wave has loaded a share
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    __syncthreads();
+    if (ragged && st == nst - 1) {
+      mask_tail(st);
+      __syncthreads();
     }
+  };
+
+  // ---- LDS to registers -----------------------------------------------------
+  // Pieces g4 and 4 + g4 of a line: any order of the features will do, if it is
+  // the same for both operands.
+  const int slot0 = 16 * (g4 ^ (i16 & 7));
+  const int xline = 16 * NX * wr + i16, wline = 64 * wc + i16;
+  auto operand = [&](const uint8_t* lines, int line, u4 (&v)[2]) {
+    v[0] = *reinterpret_cast<const u4*>(lines + 128 * line + slot0);
+    v[1] = *reinterpret_cast<const u4*>(lines + 128 * line + (slot0 ^ 64));
+  };
+  auto xscale = [&](int st, int x) { return sxs[(st >> 2) & 1][xline + 16 * x] >> (8 * (st & 3)); };
+  // scales of a lane's four channels
+  auto wscales = [&](int st, SplitScale (&s)[4]) {
+    const u4 w = *reinterpret_cast<const u4*>(&sws[(st >> 2) & 1][bytes ? 0 : st & 3][64 * wc + 4 * i16]);
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+      s[y] = split_scale(bytes ? from_e8m0((w[y] >> (8 * (st & 3))) & 0xffu) : __uint_as_float(w[y]));
   };
 
   v4 acc[NX][4];
@@ -187,54 +214,47 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
 #pragma unroll
     for (int y = 0; y < 4; ++y) acc[x][y] = v4{0.f, 0.f, 0.f, 0.f};
 
-  // chunks g4 and 4 + g4 of line l: any order of the features will do, if it
-  // is the same for both operands
-  const int slot0 = 16 * (g4 ^ (i16 & 7));
-  const int xline = 16 * NX * wr + i16, wline = 64 * wc + i16;
-  auto operand = [&](const uint8_t* lines, int line, u4 (&v)[2]) {
-    v[0] = *reinterpret_cast<const u4*>(lines + 128 * line + slot0);
-    v[1] = *reinterpret_cast<const u4*>(lines + 128 * line + (slot0 ^ 64));
-  };
-
-  load(0, 0);
-  fetch_scales(0);
-  put_scales(0);
-  __builtin_amdgcn_s_waitcnt(0x0f70);
-  __syncthreads();
-  for (int st = 0; st < nst; ++st) {
-    const int cur = st & 1, sq = (st >> 2) & 1;
-    if (128 * (int64_t)(st + 1) > a.m) {
-      mask_tail(st, cur);
-      __syncthreads();
-    }
-    if (st + 1 < nst) load(st + 1, cur ^ 1);
-    if ((st & 3) == 0 && st + 4 < nst) fetch_scales(st / 4 + 1);
-    if ((st & 3) == 3 && st + 1 < nst) put_scales(sq ^ 1);
-    __builtin_amdgcn_sched_barrier(0);
-    float s[4], power[4];
-#pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      const SplitScale sp = split_scale(sws[sq][st & 3][wline + 16 * y]);
-      s[y] = sp.rest;
-      power[y] = sp.power;
-    }
-    const int byte = 8 * (st & 3);
-    if constexpr (EXACT) {
+  load_scales(0);
+  load_w(0);
+  load_x(0);
+  if (nst > 1) {
+    load_w(1);
+    load_x(1);
+  }
+  arrived(0);
+  if constexpr (EXACT) {
+    for (int st = 0; st < nst; ++st) {
+      if ((st & 3) == 0 && st + 4 < nst) load_scales(st / 4 + 1);
+      float s[4];
       b8 fw[4][4];
+      {
+        SplitScale sp[4];
+        wscales(st, sp);
 #pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        u4 v[2];
-        operand(sW[cur], wline + 16 * y, v);
+        for (int y = 0; y < 4; ++y) {
+          s[y] = sp[y].rest;
+          u4 v[2];
+          operand(sW[st & 1], wline + 16 * y, v);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) fw[y][k] = to_bf16(v[k >> 1][2 * (k & 1)], v[k >> 1][2 * (k & 1) + 1], power[y]);
+          for (int k = 0; k < 4; ++k)
+            fw[y][k] = to_bf16(v[k >> 1][2 * (k & 1)], v[k >> 1][2 * (k & 1) + 1], sp[y].power);
+        }
       }
       u4 next[2];
-      operand(sX[cur], xline, next);
+      operand(sX[st & 1], xline, next);
 #pragma unroll
       for (int x = 0; x < NX; ++x) {
         const u4 v[2] = {next[0], next[1]};
-        if (x + 1 < NX) operand(sX[cur], xline + 16 * (x + 1), next);
-        const float sx = from_e8m0((sxs[sq][xline + 16 * x] >> byte) & 0xffu);
+        const float sx = from_e8m0(xscale(st, x) & 0xffu);
+        if (x + 1 < NX) {
+          operand(sX[st & 1], xline + 16 * (x + 1), next);
+        } else if (st + 1 < nst) {
+          arrived(st + 1);
+          if (st + 2 < nst) {
+            load_w(st + 2);
+            load_x(st + 2);
+          }
+        }
         v4 d[4];
 #pragma unroll
         for (int y = 0; y < 4; ++y) d[y] = v4{0.f, 0.f, 0.f, 0.f};
@@ -246,42 +266,94 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
             d[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx, fw[y][k], d[y], 0, 0, 0);
         }
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
+        for (int y = 0; y < 4; ++y) {
 #pragma unroll
           for (int r = 0; r < 4; ++r) acc[x][y][r] = __builtin_fmaf(d[y][r], s[y], acc[x][y][r]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    } else {
-      i8 fw[4];
-      auto eight = [](const u4 (&v)[2]) {
-        return __builtin_bit_cast(i8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
-      };
-#pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        u4 v[2];
-        operand(sW[cur], wline + 16 * y, v);
-        fw[y] = eight(v);
-      }
-      u4 next[2];
-      operand(sX[cur], xline, next);
-#pragma unroll
-      for (int x = 0; x < NX; ++x) {
-        const i8 fx = eight(next);
-        if (x + 1 < NX) operand(sX[cur], xline + 16 * (x + 1), next);
-        const int sx = (int)(sxs[sq][xline + 16 * x] >> byte);
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const v4 d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-              fx, fw[y], v4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, sx, 0,
-              (int)(__float_as_uint(power[y]) >> 23));
-#pragma unroll
-          for (int r = 0; r < 4; ++r) acc[x][y][r] = __builtin_fmaf(d[r], s[y], acc[x][y][r]);
+          pin(acc[x][y]);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    __builtin_amdgcn_s_waitcnt(0x0f70);
-    __syncthreads();
+  } else {
+    // A product's sums take their scale two products later, beside the matrix
+    // cores; the last two of a stage in the next one.  A stage's last line of
+    // activations is read ahead, so the barrier stands before its products:
+    // behind it the stage's buffers take the stage after the next, and the next
+    // stage's first operands are read.
+    auto eight = [](const u4 (&v)[2]) {
+      return __builtin_bit_cast(i8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    i8 fw[4];
+    u4 next[2];
+    float s[4], last_s[2] = {0.f, 0.f};
+    v4 wait[2] = {v4{0.f, 0.f, 0.f, 0.f}, v4{0.f, 0.f, 0.f, 0.f}};
+    uint32_t nsx;
+    auto read_w = [&](int st, int y) {
+      u4 v[2];
+      operand(sW[st & 1], wline + 16 * y, v);
+      fw[y] = eight(v);
+    };
+    auto read_x = [&](int st, int x) {
+      operand(sX[st & 1], xline + 16 * x, next);
+      nsx = xscale(st, x);
+    };
+#pragma unroll
+    for (int y = 0; y < 4; ++y) read_w(0, y);
+    read_x(0, 0);
+    for (int st = 0; st < nst; ++st) {
+      if ((st & 3) == 0 && st + 4 < nst) load_scales(st / 4 + 1);
+      uint32_t power = 0;   // four e8m0 codes
+      {
+        SplitScale sp[4];
+        wscales(st, sp);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          s[y] = sp[y].rest;
+          power |= (__float_as_uint(sp[y].power) >> 23) << (8 * y);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int x = 0; x < NX; ++x) {
+        const i8 fx = eight(next);
+        const int sx = (int)nsx;
+        if (x + 1 < NX) {
+          read_x(st, x + 1);
+        } else {
+          // (behind the last stage these read what stands there, unused)
+          if (st + 1 < nst) arrived(st + 1);
+          read_x(st + 1, 0);
+        }
+        if (x == 0 && st > 0 && st + 1 < nst) load_x(st + 1);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          constexpr v4 kZero = {0.f, 0.f, 0.f, 0.f};
+          v4 d;
+          if (y == 0) d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx, fw[0], kZero, 0, 0, 0, sx, 0, (int)power);
+          else if (y == 1) d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx, fw[1], kZero, 0, 0, 0, sx, 1, (int)power);
+          else if (y == 2) d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx, fw[2], kZero, 0, 0, 0, sx, 2, (int)power);
+          else d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx, fw[3], kZero, 0, 0, 0, sx, 3, (int)power);
+          if (x + 1 == NX) read_w(st + 1, y);
+          // (the product before the one before)
+          const int px = y >= 2 ? x : (x + NX - 1) % NX, py = (y + 2) & 3;
+          const float ps = x == 0 && y < 2 ? last_s[y] : s[py];
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            acc[px][py][r] = __builtin_fmaf(wait[y & 1][r], ps, acc[px][py][r]);
+          pin(acc[px][py]);
+          wait[y & 1] = d;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (x + 1 == NX && st + 2 < nst) load_w(st + 2);
+      }
+      last_s[0] = s[2];
+      last_s[1] = s[3];
+    }
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        acc[NX - 1][2 + y][r] = __builtin_fmaf(wait[y][r], last_s[y], acc[NX - 1][2 + y][r]);
   }
 
   // lane l holds tokens 4 g4 + r (lines) of channel i16 of each 16 x 16 block

@@ -2,6 +2,7 @@
 // fp8_matmul.hip).
 #pragma once
 
+#include "device.h"
 #include "fp8.h"
 
 namespace ojbkq {
@@ -14,6 +15,12 @@ typedef float v4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u2v __attribute__((ext_vector_type(2)));
 
+// 4 bytes per lane straight to LDS, lane i's at lds + 4 i (load_to_lds16_at's
+// narrow form).
+__device__ __forceinline__ void load_to_lds4_at(const void* src, const void* lds) {
+  const uint32_t a = __builtin_amdgcn_readfirstlane(lds_address(lds));
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "{m0}"(a) : "memory");
+}
 // 2^(code - 127) (code 0: 2^-127, the one below float32's normal range).
 __device__ __forceinline__ float from_e8m0(uint32_t code) {
   const uint32_t b = code << 23;
