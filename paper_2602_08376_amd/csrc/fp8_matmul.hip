@@ -91,16 +91,20 @@ __device__ __forceinline__ void store_run(E* p, const float (&v)[N], int64_t lef
 // 2) + i % 4, line 16 y + i of a wave's 64 of weights channel 4 i + y: a lane
 // then ends up with runs of 8 tokens and of 4 channels, whichever is contiguous
 // in Y.
-// EXACT: operands brought to bf16 (with the activations' scales, exactly) and
-// multiplied there.  Otherwise v_mfma_scale_f32_16x16x128_f8f6f4 takes them as
-// they are, scales included, at twice the rate.
-template <int NX, bool EXACT>
+// kExact: operands brought to bf16, with the activations' scales and the powers
+// of two of the weights', exactly, and multiplied there.  Otherwise
+// v_mfma_scale_f32_16x16x128_f8f6f4 takes them as they are, with these scales,
+// at twice the rate; kPowers: the weights' scales are powers of two, so it takes
+// the sums so far as well.
+enum { kPowers, kScaled, kExact };
+template <int NX, int HOW>
 __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, int64_t tiles_n) {
   constexpr int kTile = 32 * NX;
   __shared__ __align__(16) uint8_t sX[2][kTile * 128], sW[2][kTile * 128];
   // scales of four stages: of a line of activations (a byte each), of a channel
   // of weights (a float32 each, or e8m0 bytes in the first)
   __shared__ __align__(16) uint32_t sxs[2][kTile], sws[2][4][kTile];
+  __shared__ __align__(16) uint8_t swp[2][4][kTile];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i16 = lane & 15, g4 = lane >> 4;
@@ -118,31 +122,36 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
 
   // ---- memory to LDS --------------------------------------------------------
   // Load q of a wave fills lines 8 (4 wave + q) .. + 7; rows past the last one
-  // repeat it (they feed only results that are not stored).  The four rows of a
-  // lane, each below 256, share a register.
-  uint32_t xrows = 0, wrows = 0;
+  // repeat it (they feed only results that are not stored).
   const int last_t = (int)(a.T - 1 - T0 < kTile - 1 ? a.T - 1 - T0 : kTile - 1);
   const int last_j = (int)(a.n - 1 - J0 < kTile - 1 ? a.n - 1 - J0 : kTile - 1);
+  const uint32_t piece = 16 * ((lane & 7) ^ (lane >> 3));
+  uint32_t xoff[4], woff[4];
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const int line = 8 * (4 * wave + q) + (lane >> 3);
     const int t = token_of(line), j = channel_of(line);
-    xrows |= (uint32_t)(t < last_t ? t : last_t) << (8 * q);
-    wrows |= (uint32_t)(j < last_j ? j : last_j) << (8 * q);
+    xoff[q] = (uint32_t)(t < last_t ? t : last_t) * (uint32_t)a.ldx + piece;
+    woff[q] = (uint32_t)(j < last_j ? j : last_j) * (uint32_t)a.ldw + piece;
   }
   const uint8_t* const xbase = a.X8 + T0 * a.ldx;
   const uint8_t* const wbase = a.W8 + J0 * a.ldw;
-  const uint32_t piece = 16 * ((lane & 7) ^ (lane >> 3));
-  // (a piece past the last feature reads the row's first one; mask_tail clears it)
-  auto load = [&](const uint8_t* base, uint32_t rows, uint32_t ld, int st, uint8_t* to) {
-    const int64_t k0 = 128 * (int64_t)st;
-    const uint32_t at = k0 + piece < a.m ? piece : 0u;
+  const bool ragged = (a.m & 127) != 0;
+  auto load = [&](const uint8_t* base, const uint32_t (&off)[4], int st, uint8_t* to) {
+    base += 128 * (int64_t)st;
+    to += 4096 * wave;
+    if (ragged && st == nst - 1) {
+      // a piece past the last feature reads the row's first one; mask_tail clears it
+      const uint32_t back = 128 * (int64_t)st + piece < a.m ? 0u : piece;
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      load_to_lds16(base + k0, __builtin_amdgcn_ubfe(rows, 8 * q, 8) * ld + at, to + 1024 * (4 * wave + q));
+      for (int q = 0; q < 4; ++q) load_to_lds16(base, off[q] - back, to + 1024 * q);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) load_to_lds16(base, off[q], to + 1024 * q);
+    }
   };
-  auto load_x = [&](int st) { load(xbase, xrows, (uint32_t)a.ldx, st, sX[st & 1]); };
-  auto load_w = [&](int st) { load(wbase, wrows, (uint32_t)a.ldw, st, sW[st & 1]); };
+  auto load_x = [&](int st) { load(xbase, xoff, st, sX[st & 1]); };
+  auto load_w = [&](int st) { load(wbase, woff, st, sW[st & 1]); };
   // the last stage of a ragged row: everything from feature m on cleared
   auto mask_tail = [&](int st) {
     const int left = (int)(a.m - 128 * (int64_t)st);
@@ -180,7 +189,6 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
       }
     }
   };
-  const bool ragged = (a.m & 127) != 0;
   auto arrived = [&](int st) {   // stage st, of which every wave has loaded a share
     __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();
@@ -199,13 +207,31 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
     v[0] = *reinterpret_cast<const u4*>(lines + 128 * line + slot0);
     v[1] = *reinterpret_cast<const u4*>(lines + 128 * line + (slot0 ^ 64));
   };
-  auto xscale = [&](int st, int x) { return sxs[(st >> 2) & 1][xline + 16 * x] >> (8 * (st & 3)); };
-  // scales of a lane's four channels
-  auto wscales = [&](int st, SplitScale (&s)[4]) {
-    const u4 w = *reinterpret_cast<const u4*>(&sws[(st >> 2) & 1][bytes ? 0 : st & 3][64 * wc + 4 * i16]);
+  auto xscales = [&](int st, int x) { return sxs[(st >> 2) & 1][xline + 16 * x]; };   // of four stages
+  // The scales of four stages parted in place (split_scale), a thread to a
+  // channel, well before the first of them.
+  auto part_scales = [&](int quad) {
+    if (wave < kTile / 64) return;
+    const int c = tid - kTile, buf = quad & 1;
+    const uint32_t first = sws[buf][0][c];
 #pragma unroll
-    for (int y = 0; y < 4; ++y)
-      s[y] = split_scale(bytes ? from_e8m0((w[y] >> (8 * (st & 3))) & 0xffu) : __uint_as_float(w[y]));
+    for (int e = 0; e < 4; ++e) {
+      if (HOW == kPowers) {
+        swp[buf][e][c] = (uint8_t)(first >> (8 * e));
+        continue;
+      }
+      const uint32_t w = sws[buf][e][c];
+      const SplitScale sp = split_scale(bytes ? from_e8m0((first >> (8 * e)) & 0xffu) : __uint_as_float(w));
+      sws[buf][e][c] = __float_as_uint(sp.rest);
+      swp[buf][e][c] = (uint8_t)(__float_as_uint(sp.power) >> 23);
+    }
+  };
+  // of a lane's four channels
+  auto rests = [&](int st) {
+    return *reinterpret_cast<const v4*>(&sws[(st >> 2) & 1][st & 3][64 * wc + 4 * i16]);
+  };
+  auto powers = [&](int st) {
+    return *reinterpret_cast<const uint32_t*>(&swp[(st >> 2) & 1][st & 3][64 * wc + 4 * i16]);
   };
 
   v4 acc[NX][4];
@@ -222,32 +248,34 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
     load_x(1);
   }
   arrived(0);
-  if constexpr (EXACT) {
+  part_scales(0);
+  __syncthreads();
+  if constexpr (HOW == kExact) {
     for (int st = 0; st < nst; ++st) {
       if ((st & 3) == 0 && st + 4 < nst) load_scales(st / 4 + 1);
-      float s[4];
+      if ((st & 3) == 1 && (st | 3) + 1 < nst) part_scales(st / 4 + 1);
+      const v4 s = rests(st);
+      const uint32_t power = powers(st);
       b8 fw[4][4];
-      {
-        SplitScale sp[4];
-        wscales(st, sp);
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          s[y] = sp[y].rest;
-          u4 v[2];
-          operand(sW[st & 1], wline + 16 * y, v);
+      for (int y = 0; y < 4; ++y) {
+        u4 v[2];
+        operand(sW[st & 1], wline + 16 * y, v);
+        const float p = __uint_as_float(((power >> (8 * y)) & 0xffu) << 23);
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            fw[y][k] = to_bf16(v[k >> 1][2 * (k & 1)], v[k >> 1][2 * (k & 1) + 1], sp[y].power);
-        }
+        for (int k = 0; k < 4; ++k)
+          fw[y][k] = to_bf16(v[k >> 1][2 * (k & 1)], v[k >> 1][2 * (k & 1) + 1], p);
       }
       u4 next[2];
       operand(sX[st & 1], xline, next);
+      uint32_t nsx = xscales(st, 0);
 #pragma unroll
       for (int x = 0; x < NX; ++x) {
         const u4 v[2] = {next[0], next[1]};
-        const float sx = from_e8m0(xscale(st, x) & 0xffu);
+        const float sx = from_e8m0((nsx >> (8 * (st & 3))) & 0xffu);
         if (x + 1 < NX) {
           operand(sX[st & 1], xline + 16 * (x + 1), next);
+          nsx = xscales(st, x + 1);
         } else if (st + 1 < nst) {
           arrived(st + 1);
           if (st + 2 < nst) {
@@ -285,7 +313,9 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
     };
     i8 fw[4];
     u4 next[2];
-    float s[4], last_s[2] = {0.f, 0.f};
+    v4 s = rests(0);
+    uint32_t power = powers(0), next_power = 0;   // four e8m0 codes
+    float last_s[2] = {0.f, 0.f};
     v4 wait[2] = {v4{0.f, 0.f, 0.f, 0.f}, v4{0.f, 0.f, 0.f, 0.f}};
     uint32_t nsx;
     auto read_w = [&](int st, int y) {
@@ -295,28 +325,19 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
     };
     auto read_x = [&](int st, int x) {
       operand(sX[st & 1], xline + 16 * x, next);
-      nsx = xscale(st, x);
+      nsx = xscales(st, x);
     };
 #pragma unroll
     for (int y = 0; y < 4; ++y) read_w(0, y);
     read_x(0, 0);
     for (int st = 0; st < nst; ++st) {
       if ((st & 3) == 0 && st + 4 < nst) load_scales(st / 4 + 1);
-      uint32_t power = 0;   // four e8m0 codes
-      {
-        SplitScale sp[4];
-        wscales(st, sp);
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          s[y] = sp[y].rest;
-          power |= (__float_as_uint(sp[y].power) >> 23) << (8 * y);
-        }
-      }
+      if ((st & 3) == 1 && (st | 3) + 1 < nst) part_scales(st / 4 + 1);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int x = 0; x < NX; ++x) {
         const i8 fx = eight(next);
-        const int sx = (int)nsx;
+        const int sx = (int)(nsx >> (8 * (st & 3)));
         if (x + 1 < NX) {
           read_x(st, x + 1);
         } else {
@@ -324,16 +345,23 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
           if (st + 1 < nst) arrived(st + 1);
           read_x(st + 1, 0);
         }
+        if (x == NX / 2) next_power = powers(st + 1);
         if (x == 0 && st > 0 && st + 1 < nst) load_x(st + 1);
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
           constexpr v4 kZero = {0.f, 0.f, 0.f, 0.f};
-          v4 d;
-          if (y == 0) d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx, fw[0], kZero, 0, 0, 0, sx, 0, (int)power);
-          else if (y == 1) d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx, fw[1], kZero, 0, 0, 0, sx, 1, (int)power);
-          else if (y == 2) d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx, fw[2], kZero, 0, 0, 0, sx, 2, (int)power);
-          else d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx, fw[3], kZero, 0, 0, 0, sx, 3, (int)power);
+          v4 d = HOW == kPowers ? acc[x][y] : kZero;
+          if (y == 0) d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx, fw[0], d, 0, 0, 0, sx, 0, (int)power);
+          else if (y == 1) d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx, fw[1], d, 0, 0, 0, sx, 1, (int)power);
+          else if (y == 2) d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx, fw[2], d, 0, 0, 0, sx, 2, (int)power);
+          else d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fx, fw[3], d, 0, 0, 0, sx, 3, (int)power);
           if (x + 1 == NX) read_w(st + 1, y);
+          if (HOW == kPowers) {
+            acc[x][y] = d;
+            pin(acc[x][y]);
+            __builtin_amdgcn_sched_barrier(0);
+            continue;
+          }
           // (the product before the one before)
           const int px = y >= 2 ? x : (x + NX - 1) % NX, py = (y + 2) & 3;
           const float ps = x == 0 && y < 2 ? last_s[y] : s[py];
@@ -348,9 +376,11 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
       }
       last_s[0] = s[2];
       last_s[1] = s[3];
+      s = rests(st + 1);
+      power = next_power;
     }
 #pragma unroll
-    for (int y = 0; y < 2; ++y)
+    for (int y = 0; y < (HOW == kPowers ? 0 : 2); ++y)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
         acc[NX - 1][2 + y][r] = __builtin_fmaf(wait[y][r], last_s[y], acc[NX - 1][2 + y][r]);
@@ -392,8 +422,9 @@ hipError_t launch_tiles(const Product8Args& a, hipStream_t s) {
   const int64_t tiles_n = (a.n + kTile - 1) / kTile, tiles = tiles_n * ((a.T + kTile - 1) / kTile);
   if (tiles > 0x7fffffff) return hipErrorInvalidValue;
   const dim3 grid((unsigned)tiles), block(64 * NX);
-  if (a.ytype == 0) product8_kernel<NX, true><<<grid, block, 0, s>>>(a, tiles_n);
-  else product8_kernel<NX, false><<<grid, block, 0, s>>>(a, tiles_n);
+  if (a.ytype == 0) product8_kernel<NX, kExact><<<grid, block, 0, s>>>(a, tiles_n);
+  else if (a.ws_e8m0) product8_kernel<NX, kPowers><<<grid, block, 0, s>>>(a, tiles_n);
+  else product8_kernel<NX, kScaled><<<grid, block, 0, s>>>(a, tiles_n);
   return hipGetLastError();
 }
 
