@@ -5,12 +5,6 @@
 namespace ojbkq {
 namespace {
 
-// All but the youngest N of the wave's loads have arrived.
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-  static_assert(N < 64, "six bits");
-  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
-}
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
 
 // Y for few tokens.  Bound by reading the weights (for the fewest tokens by

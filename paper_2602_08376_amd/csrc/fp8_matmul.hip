@@ -14,20 +14,28 @@ typedef int i8 __attribute__((ext_vector_type(8)));
 // ---- codes in e4m3 ---------------------------------------------------------
 
 // W8 [n, ldw] e4m3 = q - z of the packed codes: whole numbers of at most 15,
-// exact in e4m3's 4 significant bits.  One thread to 32 codes (BITS words of a
-// row).  Bound by memory: it writes a byte for every code.
+// exact in e4m3's 4 significant bits.  One thread to 32 codes (BITS words) of
+// a row, and of others below it.  Bound by memory: it writes a byte for every code.
 template <int BITS>
 __global__ __launch_bounds__(256) void expand_codes_kernel(Product8Args a, uint8_t* W8, int64_t ldw) {
-  const int64_t runs = ldw / 32, total = a.n * runs;
-  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < total; e += (int64_t)gridDim.x * 256) {
-    const int64_t j = e / runs, u = e % runs;
-    const uint32_t* const row = a.P + j * a.wpr;
+  const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;   // 32 codes of a row
+  if (32 * u >= ldw) return;
+  // (runs past the last feature: any group will do, they are not used)
+  const uint32_t grp = 32 * u < a.m ? (uint32_t)(u / 4) / a.ws_div : 0u;
+  const bool whole = (u + 1) * BITS <= a.wpr;
+  for (int64_t j = blockIdx.y; j < a.n; j += gridDim.y) {
+    const uint32_t* const row = a.P + j * a.wpr + u * BITS;
     uint32_t w[BITS];
+    if (whole) {
+      typedef uint32_t Any __attribute__((ext_vector_type(BITS), aligned(4)));
+      const Any v = *reinterpret_cast<const Any*>(row);
 #pragma unroll
-    for (int q = 0; q < BITS; ++q) w[q] = row[u * BITS + q < a.wpr ? u * BITS + q : a.wpr - 1];
-    // (runs past the last feature: any group will do, they are not used)
-    const uint32_t b = 32 * u < a.m ? (uint32_t)(u / 4) : 0u;
-    const float z = whole_zero<BITS>(a.Z[j * a.ws_ld + b / a.ws_div]);
+      for (int q = 0; q < BITS; ++q) w[q] = v[q];
+    } else {
+#pragma unroll
+      for (int q = 0; q < BITS; ++q) w[q] = u * BITS + q < a.wpr ? row[q] : 0u;
+    }
+    const float z = whole_zero<BITS>(a.Z[j * a.ws_ld + grp]);
     u4 out[2];
 #pragma unroll
     for (int d = 0; d < 8; ++d) {
@@ -81,12 +89,12 @@ __device__ __forceinline__ void store_run(E* p, const float (&v)[N], int64_t lef
   }
 }
 
-// Tiles of kTile tokens x kTile channels (256 with eight waves, 128 with four),
-// a block of 128 features to a stage, two stages in LDS.  A wave holds 16 NX
-// tokens x 64 channels: its weights of a stage stay in registers while its
-// activations pass.  Both operands go straight from memory to LDS in lines of
-// 128 bytes, 16-byte chunk c of line l at slot c ^ (l % 8), which spreads the
-// operand reads of 16 lines x 4 chunks over all banks.
+// Tiles of TT tokens x TC channels, a block of 128 features to a stage, BUFS
+// stages in LDS; WR x WC waves, each of 16 NX tokens x 64 channels: its weights
+// of a stage stay in registers while its activations pass.  Both operands go
+// straight from memory to LDS in lines of 128 bytes, 16-byte chunk c of line l
+// at slot c ^ (l % 8), which spreads the operand reads of 16 lines x 4 chunks
+// over all banks.
 // Line 16 x + i of the activations holds token 32 (x / 2) + 8 (i / 4) + 4 (x %
 // 2) + i % 4, line 16 y + i of a wave's 64 of weights channel 4 i + y: a lane
 // then ends up with runs of 8 tokens and of 4 channels, whichever is contiguous
@@ -97,21 +105,22 @@ __device__ __forceinline__ void store_run(E* p, const float (&v)[N], int64_t lef
 // at twice the rate; kPowers: the weights' scales are powers of two, so it takes
 // the sums so far as well.
 enum { kPowers, kScaled, kExact };
-template <int NX, int HOW>
-__global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, int64_t tiles_n) {
-  constexpr int kTile = 32 * NX;
-  __shared__ __align__(16) uint8_t sX[2][kTile * 128], sW[2][kTile * 128];
+template <int TT, int TC, int WR, int WC, int BUFS, int HOW>
+__global__ __launch_bounds__(64 * WR * WC, 2) void product8_kernel(Product8Args a, int64_t tiles_n) {
+  constexpr int NX = TT / WR / 16, kWaves = WR * WC, kLines = TT + TC;
+  static_assert(TC == 64 * WC && NX % 2 == 0 && kLines <= 64 * kWaves && TT <= 256 && TC <= 256, "");
+  __shared__ __align__(16) uint8_t sX[BUFS][TT * 128], sW[BUFS][TC * 128];
   // scales of four stages: of a line of activations (a byte each), of a channel
   // of weights (a float32 each, or e8m0 bytes in the first)
-  __shared__ __align__(16) uint32_t sxs[2][kTile], sws[2][4][kTile];
-  __shared__ __align__(16) uint8_t swp[2][4][kTile];
+  __shared__ __align__(16) uint32_t sxs[2][TT], sws[2][4][TC];
+  __shared__ __align__(16) uint8_t swp[2][4][TC];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i16 = lane & 15, g4 = lane >> 4;
-  const int wr = wave & 1, wc = wave >> 1;
+  const int wr = wave % WR, wc = wave / WR;
   int64_t tj, tt;
   tile_of(tiles_n, tj, tt);
-  const int64_t J0 = tj * kTile, T0 = tt * kTile;
+  const int64_t J0 = tj * TC, T0 = tt * TT;
   const int nst = (int)((a.m + 127) / 128);
 
   auto token_of = [](int line) {
@@ -121,41 +130,41 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
   auto channel_of = [](int line) { return (line & ~63) + 4 * (line & 15) + ((line >> 4) & 3); };
 
   // ---- memory to LDS --------------------------------------------------------
-  // Load q of a wave fills lines 8 (4 wave + q) .. + 7; rows past the last one
+  // Load q of a wave fills lines 8 (QX wave + q) .. + 7; rows past the last one
   // repeat it (they feed only results that are not stored).
-  const int last_t = (int)(a.T - 1 - T0 < kTile - 1 ? a.T - 1 - T0 : kTile - 1);
-  const int last_j = (int)(a.n - 1 - J0 < kTile - 1 ? a.n - 1 - J0 : kTile - 1);
+  constexpr int QX = TT / 8 / kWaves, QW = TC / 8 / kWaves;
+  const int last_t = (int)(a.T - 1 - T0 < TT - 1 ? a.T - 1 - T0 : TT - 1);
+  const int last_j = (int)(a.n - 1 - J0 < TC - 1 ? a.n - 1 - J0 : TC - 1);
   const uint32_t piece = 16 * ((lane & 7) ^ (lane >> 3));
-  uint32_t xoff[4], woff[4];
+  uint32_t xoff[QX], woff[QW];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int line = 8 * (4 * wave + q) + (lane >> 3);
-    const int t = token_of(line), j = channel_of(line);
+  for (int q = 0; q < QX; ++q) {
+    const int t = token_of(8 * (QX * wave + q) + (lane >> 3));
     xoff[q] = (uint32_t)(t < last_t ? t : last_t) * (uint32_t)a.ldx + piece;
+  }
+#pragma unroll
+  for (int q = 0; q < QW; ++q) {
+    const int j = channel_of(8 * (QW * wave + q) + (lane >> 3));
     woff[q] = (uint32_t)(j < last_j ? j : last_j) * (uint32_t)a.ldw + piece;
   }
   const uint8_t* const xbase = a.X8 + T0 * a.ldx;
   const uint8_t* const wbase = a.W8 + J0 * a.ldw;
   const bool ragged = (a.m & 127) != 0;
-  auto load = [&](const uint8_t* base, const uint32_t (&off)[4], int st, uint8_t* to) {
-    base += 128 * (int64_t)st;
-    to += 4096 * wave;
-    if (ragged && st == nst - 1) {
-      // a piece past the last feature reads the row's first one; mask_tail clears it
-      const uint32_t back = 128 * (int64_t)st + piece < a.m ? 0u : piece;
+  auto load = [&](int st) {
+    const int64_t k0 = 128 * (int64_t)st;
+    const int buf = st % BUFS;
+    // a piece past the last feature reads the row's first one; mask_tail clears it
+    const uint32_t back = ragged && st == nst - 1 && k0 + piece >= a.m ? piece : 0u;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) load_to_lds16(base, off[q] - back, to + 1024 * q);
-    } else {
+    for (int q = 0; q < QW; ++q) load_to_lds16(wbase + k0, woff[q] - back, sW[buf] + 1024 * (QW * wave + q));
 #pragma unroll
-      for (int q = 0; q < 4; ++q) load_to_lds16(base, off[q], to + 1024 * q);
-    }
+    for (int q = 0; q < QX; ++q) load_to_lds16(xbase + k0, xoff[q] - back, sX[buf] + 1024 * (QX * wave + q));
   };
-  auto load_x = [&](int st) { load(xbase, xoff, st, sX[st & 1]); };
-  auto load_w = [&](int st) { load(wbase, woff, st, sW[st & 1]); };
   // the last stage of a ragged row: everything from feature m on cleared
   auto mask_tail = [&](int st) {
-    const int left = (int)(a.m - 128 * (int64_t)st);
-    uint8_t* const line = (tid < kTile ? sX[st & 1] : sW[st & 1]) + 128 * (tid & (kTile - 1));
+    if (tid >= kLines) return;
+    const int left = (int)(a.m - 128 * (int64_t)st), buf = st % BUFS;
+    uint8_t* const line = tid < TT ? sX[buf] + 128 * tid : sW[buf] + 128 * (tid - TT);
     for (int c = left / 16; c < 8; ++c) {
       u4* const p = reinterpret_cast<u4*>(line + 16 * (c ^ (tid & 7)));
       u4 v = *p;
@@ -171,11 +180,11 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
     int w = wave;
     __asm__("" : "+s"(w));
     const int buf = quad & 1;
-    if (w < kTile / 64) {
+    if (w < TT / 64) {
       const int t = token_of(64 * w + lane);
       load_to_lds4_at(a.xs + (T0 + (t < last_t ? t : last_t)) * a.lds + 4 * quad, &sxs[buf][64 * w]);
-    } else {
-      const int c0 = 64 * (w - kTile / 64), j = c0 + lane;
+    } else if (w < kLines / 64) {
+      const int c0 = 64 * (w - TT / 64), j = c0 + lane;
       const int64_t at = ((J0 + (j < last_j ? j : last_j)) >> a.ws_shift) * a.ws_ld;
       const uint8_t* const S = static_cast<const uint8_t*>(a.ws);
       if (bytes) {
@@ -189,8 +198,11 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
       }
     }
   };
-  auto arrived = [&](int st) {   // stage st, of which every wave has loaded a share
-    __builtin_amdgcn_s_waitcnt(0x0f70);
+  // Stage st, of which every wave has loaded a share, has arrived (the youngest
+  // loads are those of the stages behind it); at the end of the stage before.
+  auto arrived = [&](int st) {
+    if (BUFS > 2 && st + 1 < nst) wait_loads<(BUFS - 2) * (QX + QW)>();
+    else wait_loads<0>();
     __syncthreads();
     if (ragged && st == nst - 1) {
       mask_tail(st);
@@ -211,8 +223,8 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
   // The scales of four stages parted in place (split_scale), a thread to a
   // channel, well before the first of them.
   auto part_scales = [&](int quad) {
-    if (wave < kTile / 64) return;
-    const int c = tid - kTile, buf = quad & 1;
+    if (tid < TT || tid >= kLines) return;
+    const int c = tid - TT, buf = quad & 1;
     const uint32_t first = sws[buf][0][c];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -241,67 +253,95 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
     for (int y = 0; y < 4; ++y) acc[x][y] = v4{0.f, 0.f, 0.f, 0.f};
 
   load_scales(0);
-  load_w(0);
-  load_x(0);
-  if (nst > 1) {
-    load_w(1);
-    load_x(1);
-  }
+#pragma unroll
+  for (int st = 0; st < BUFS - 1; ++st)
+    if (st < nst) load(st);
+  wait_loads<0>();
   arrived(0);
   part_scales(0);
   __syncthreads();
   if constexpr (HOW == kExact) {
+    // The sums take their scale beside the products of the next line of
+    // activations (the last one's beside the next stage's first); the barrier
+    // stands before a stage's last line, behind it the weights of the next stage
+    // are read and brought to bf16 as the last products leave them.
+    b8 fw[4][4];
+    u4 next[2], wnext[4];
+    uint32_t nsx;
+    v4 s = rests(0), last_s = {0.f, 0.f, 0.f, 0.f}, wait[4];
+    uint32_t power = powers(0);
+    auto read_x = [&](int st, int x) {
+      operand(sX[st % BUFS], xline + 16 * x, next);
+      nsx = xscales(st, x);
+    };
+    // half h of the weights of a stage (products 2 h and 2 h + 1)
+    auto read_w = [&](int st, int h) {
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        wnext[y] = *reinterpret_cast<const u4*>(sW[st % BUFS] + 128 * (wline + 16 * y) + (slot0 ^ (64 * h)));
+    };
+    auto bring_w = [&](uint32_t codes, int k) {
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        fw[y][k] = to_bf16(wnext[y][2 * (k & 1)], wnext[y][2 * (k & 1) + 1],
+                           __uint_as_float(((codes >> (8 * y)) & 0xffu) << 23));
+    };
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      read_w(0, h);
+      bring_w(power, 2 * h);
+      bring_w(power, 2 * h + 1);
+    }
+    read_x(0, 0);
+#pragma unroll
+    for (int y = 0; y < 4; ++y) wait[y] = v4{0.f, 0.f, 0.f, 0.f};
     for (int st = 0; st < nst; ++st) {
       if ((st & 3) == 0 && st + 4 < nst) load_scales(st / 4 + 1);
       if ((st & 3) == 1 && (st | 3) + 1 < nst) part_scales(st / 4 + 1);
-      const v4 s = rests(st);
-      const uint32_t power = powers(st);
-      b8 fw[4][4];
-#pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        u4 v[2];
-        operand(sW[st & 1], wline + 16 * y, v);
-        const float p = __uint_as_float(((power >> (8 * y)) & 0xffu) << 23);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          fw[y][k] = to_bf16(v[k >> 1][2 * (k & 1)], v[k >> 1][2 * (k & 1) + 1], p);
-      }
-      u4 next[2];
-      operand(sX[st & 1], xline, next);
-      uint32_t nsx = xscales(st, 0);
+      if (st + BUFS - 1 < nst) load(st + BUFS - 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int x = 0; x < NX; ++x) {
         const u4 v[2] = {next[0], next[1]};
         const float sx = from_e8m0((nsx >> (8 * (st & 3))) & 0xffu);
         if (x + 1 < NX) {
-          operand(sX[st & 1], xline + 16 * (x + 1), next);
-          nsx = xscales(st, x + 1);
-        } else if (st + 1 < nst) {
-          arrived(st + 1);
-          if (st + 2 < nst) {
-            load_w(st + 2);
-            load_x(st + 2);
-          }
+          read_x(st, x + 1);
+        } else {
+          // (behind the last stage these read what stands there, unused)
+          if (st + 1 < nst) arrived(st + 1);
+          read_w(st + 1, 0);
+          read_x(st + 1, 0);
+          power = powers(st + 1);
         }
         v4 d[4];
-#pragma unroll
-        for (int y = 0; y < 4; ++y) d[y] = v4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const b8 fx = to_bf16(v[k >> 1][2 * (k & 1)], v[k >> 1][2 * (k & 1) + 1], sx);
 #pragma unroll
           for (int y = 0; y < 4; ++y)
-            d[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx, fw[y][k], d[y], 0, 0, 0);
+            d[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx, fw[y][k], k ? d[y] : v4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+          if (x + 1 == NX) {
+            bring_w(power, k);
+            if (k == 1) read_w(st + 1, 1);
+          }
+          constexpr int kLast = NX - 1;
+          const int px = x ? x - 1 : kLast;
+          const float ps = x ? s[k] : last_s[k];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[px][k][r] = __builtin_fmaf(wait[k][r], ps, acc[px][k][r]);
+          pin(acc[px][k]);
+          __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-#pragma unroll
-          for (int r = 0; r < 4; ++r) acc[x][y][r] = __builtin_fmaf(d[y][r], s[y], acc[x][y][r]);
-          pin(acc[x][y]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
+        for (int y = 0; y < 4; ++y) wait[y] = d[y];
       }
+      last_s = s;
+      s = rests(st + 1);
     }
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[NX - 1][y][r] = __builtin_fmaf(wait[y][r], last_s[y], acc[NX - 1][y][r]);
   } else {
     // A product's sums take their scale two products later, beside the matrix
     // cores; the last two of a stage in the next one.  A stage's last line of
@@ -320,11 +360,11 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
     uint32_t nsx;
     auto read_w = [&](int st, int y) {
       u4 v[2];
-      operand(sW[st & 1], wline + 16 * y, v);
+      operand(sW[st % BUFS], wline + 16 * y, v);
       fw[y] = eight(v);
     };
     auto read_x = [&](int st, int x) {
-      operand(sX[st & 1], xline + 16 * x, next);
+      operand(sX[st % BUFS], xline + 16 * x, next);
       nsx = xscales(st, x);
     };
 #pragma unroll
@@ -333,6 +373,7 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
     for (int st = 0; st < nst; ++st) {
       if ((st & 3) == 0 && st + 4 < nst) load_scales(st / 4 + 1);
       if ((st & 3) == 1 && (st | 3) + 1 < nst) part_scales(st / 4 + 1);
+      if (st + BUFS - 1 < nst) load(st + BUFS - 1);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int x = 0; x < NX; ++x) {
@@ -346,7 +387,6 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
           read_x(st + 1, 0);
         }
         if (x == NX / 2) next_power = powers(st + 1);
-        if (x == 0 && st > 0 && st + 1 < nst) load_x(st + 1);
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
           constexpr v4 kZero = {0.f, 0.f, 0.f, 0.f};
@@ -372,7 +412,6 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
           wait[y & 1] = d;
           __builtin_amdgcn_sched_barrier(0);
         }
-        if (x + 1 == NX && st + 2 < nst) load_w(st + 2);
       }
       last_s[0] = s[2];
       last_s[1] = s[3];
@@ -416,42 +455,59 @@ __global__ __launch_bounds__(64 * NX, 2) void product8_kernel(Product8Args a, in
   else store(static_cast<__bf16*>(a.Y));
 }
 
-template <int NX>
+template <int TT, int TC, int WR, int WC, int BUFS, int HOW>
 hipError_t launch_tiles(const Product8Args& a, hipStream_t s) {
-  constexpr int kTile = 32 * NX;
-  const int64_t tiles_n = (a.n + kTile - 1) / kTile, tiles = tiles_n * ((a.T + kTile - 1) / kTile);
+  const int64_t tiles_n = (a.n + TC - 1) / TC, tiles = tiles_n * ((a.T + TT - 1) / TT);
   if (tiles > 0x7fffffff) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)tiles), block(64 * NX);
-  if (a.ytype == 0) product8_kernel<NX, kExact><<<grid, block, 0, s>>>(a, tiles_n);
-  else if (a.ws_e8m0) product8_kernel<NX, kPowers><<<grid, block, 0, s>>>(a, tiles_n);
-  else product8_kernel<NX, kScaled><<<grid, block, 0, s>>>(a, tiles_n);
+  product8_kernel<TT, TC, WR, WC, BUFS, HOW>
+      <<<dim3((unsigned)tiles), dim3(64 * WR * WC), 0, s>>>(a, tiles_n);
   return hipGetLastError();
 }
 
-// Up to two workgroups of 64 channels x 64 tokens per CU, or up to 32 tokens.
-bool few(int64_t n, int64_t m, int64_t T) {
-  const int64_t blocks = (n + 63) / 64 * ((T + 63) / 64);
-  return blocks <= 512 || T <= 32;
+template <int HOW>
+hipError_t launch_how(const Product8Args& a, hipStream_t s) {
+  auto tiles = [&](int64_t tt, int64_t tc) { return (a.n + tc - 1) / tc * ((a.T + tt - 1) / tt); };
+  if constexpr (HOW == kExact) {
+    return tiles(256, 128) >= 192 ? launch_tiles<256, 128, 4, 2, 3, HOW>(a, s)
+                                  : launch_tiles<128, 128, 2, 2, 2, HOW>(a, s);
+  } else {
+    return 100 * ((tiles(256, 256) + 255) / 256) <= 62 * ((tiles(128, 128) + 511) / 512)
+               ? launch_tiles<256, 256, 2, 4, 2, HOW>(a, s)
+               : launch_tiles<128, 128, 2, 2, 2, HOW>(a, s);
+  }
+}
+
+// The kernel for few tokens takes up to 32 of them, and more while it launches
+// few workgroups (of 32 channels x 32 tokens at most): 27 us for 1000 of them at
+// m = 4096, where a round of 128-wide tiles takes 35 us however full, 48 us with
+// float32 results, and 14 or 20 us more expand the codes of 4096 and 14336
+// channels (both sides: 4096 channels, 256 tokens: 28.8 / 35.2 and codes 30.3 /
+// 49.9; 512 tokens: 53.9 / 35.9 and 56.8 / 49.4; float32 54.0 / 49.5, codes 56.0
+// / 61.9).  Both go with m.
+bool few(int64_t n, int64_t T, bool codes, bool f32) {
+  const int64_t most = codes ? (f32 ? 2304 : 1792) : (f32 ? 1792 : 1280);
+  return T <= 32 || (n + 31) / 32 * ((T + 31) / 32) <= most;
 }
 int64_t expanded_row(int64_t m) { return (m + 127) / 128 * 128; }
 
 }  // namespace
 
 size_t product8_workspace_bytes(int64_t n, int64_t m, int64_t T) {
-  return few(n, m, T) ? 0 : (size_t)n * (size_t)expanded_row(m);
+  return few(n, T, true, false) ? 0 : (size_t)n * (size_t)expanded_row(m);
 }
 
 hipError_t launch_product8(const Product8Args& a, int bits, void* workspace, hipStream_t stream) {
   // (tiles address their rows with 32 bits)
-  if (few(a.n, a.m, a.T) || a.ldx > (1 << 23) || (bits == 0 && a.ldw > (1 << 23)))
+  if (few(a.n, a.T, bits != 0, a.ytype == 0) || a.ldx > (1 << 23) || (bits == 0 && a.ldw > (1 << 23)))
     return launch_product_few8(a, bits, stream);
   Product8Args b = a;
   if (bits) {
     uint8_t* const W8 = static_cast<uint8_t*>(workspace);
     b.W8 = W8;
     b.ldw = expanded_row(a.m);
-    const int64_t blocks = (a.n * (b.ldw / 32) + 255) / 256;
-    const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536)), block(256);
+    // about eight rows to a workgroup where that leaves enough of them
+    const int64_t across = (b.ldw / 32 + 255) / 256, down = a.n * across >= 16384 ? (a.n + 7) / 8 : a.n;
+    const dim3 grid((unsigned)across, (unsigned)(down < 65535 ? down : 65535)), block(256);
     switch (bits) {
       case 1: expand_codes_kernel<1><<<grid, block, 0, stream>>>(a, W8, b.ldw); break;
       case 2: expand_codes_kernel<2><<<grid, block, 0, stream>>>(a, W8, b.ldw); break;
@@ -461,10 +517,8 @@ hipError_t launch_product8(const Product8Args& a, int bits, void* workspace, hip
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
-  const int64_t big = (b.n + 255) / 256 * ((b.T + 255) / 256);
-  const int64_t small = (b.n + 127) / 128 * ((b.T + 127) / 128);
-  return 100 * ((big + 255) / 256) <= 65 * ((small + 511) / 512) ? launch_tiles<8>(b, stream)
-                                                                 : launch_tiles<4>(b, stream);
+  if (b.ytype == 0) return launch_how<kExact>(b, stream);
+  return b.ws_e8m0 ? launch_how<kPowers>(b, stream) : launch_how<kScaled>(b, stream);
 }
 
 }  // namespace ojbkq

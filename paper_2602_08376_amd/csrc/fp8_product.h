@@ -21,6 +21,13 @@ __device__ __forceinline__ void load_to_lds4_at(const void* src, const void* lds
   const uint32_t a = __builtin_amdgcn_readfirstlane(lds_address(lds));
   asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "{m0}"(a) : "memory");
 }
+// All but the youngest N of the wave's loads have arrived.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N < 64, "six bits");
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+
 // 2^(code - 127) (code 0: 2^-127, the one below float32's normal range).
 __device__ __forceinline__ float from_e8m0(uint32_t code) {
   const uint32_t b = code << 23;

@@ -39,8 +39,8 @@ def _gpu():
 
 
 def in_tiles(n, T):
-    """Whether the sizes are beyond the kernel for few tokens."""
-    return T > 32 and -(-n // 64) * -(-T // 64) > 512
+    """Whether the sizes may be beyond the kernel for few tokens."""
+    return T > 32 and -(-n // 32) * -(-T // 32) > 1280
 
 
 def leading(v, scale):
@@ -113,7 +113,8 @@ def eight_bits(rows, m, seed, block_rows=1, pad=0, spread=2.0):
 
 SIZES = [(1, 1, 1), (5, 3, 2), (16, 128, 16), (17, 129, 1), (16, 127, 15), (33, 1000, 17), (40, 300, 7), (130, 640, 33),
          (257, 1025, 1), (64, 4096, 3), (300, 2500, 65), (8193, 256, 20), (4100, 200, 130), (16400, 136, 9),
-         (2100, 144, 1003), (600, 784, 600), (2100, 1100, 1003), (4300, 200, 4100), (4352, 1296, 4097)]
+         (2100, 144, 1003), (600, 784, 600), (2100, 1100, 1003), (4300, 200, 4100), (4352, 1296, 4097),
+         (300, 700, 4500), (33000, 260, 40)]
 
 
 @pytest.mark.parametrize("y", list(TYPES))
@@ -150,7 +151,8 @@ def codes(n, m, bits, group, seed):
                                          (33, 1000, 17, 128), (40, 300, 7, 256), (130, 640, 33, 0), (257, 1025, 1, 384),
                                          (300, 2500, 65, 128), (8193, 256, 20, 128), (16400, 136, 9, 0),
                                          (2100, 144, 1003, 128), (600, 784, 600, 256), (2100, 1100, 1003, 512),
-                                         (4352, 1296, 4097, 128), (4300, 200, 4100, 0)])
+                                         (4352, 1296, 4097, 128), (4300, 200, 4100, 0),
+                                         (33000, 260, 40, 128), (300, 700, 6500, 128)])
 @pytest.mark.parametrize("bits", [1, 2, 3, 4])
 def test_dequant_matmul(n, m, T, group, bits, y, tokens_first):
     P, S, Z, W = codes(n, m, bits, group, n + m + bits)
