@@ -458,7 +458,8 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void product8_kernel(Product8Args 
 template <int TT, int TC, int WR, int WC, int BUFS, int HOW>
 hipError_t launch_tiles(const Product8Args& a, hipStream_t s) {
   const int64_t tiles_n = (a.n + TC - 1) / TC, tiles = tiles_n * ((a.T + TT - 1) / TT);
-  if (tiles > 0x7fffffff) return hipErrorInvalidValue;
+  // (a grid holds 2^32 - 1 threads: a result beyond that is one of over 500 GB)
+  if (tiles * (64 * WR * WC) >> 32) return hipErrorInvalidValue;
   product8_kernel<TT, TC, WR, WC, BUFS, HOW>
       <<<dim3((unsigned)tiles), dim3(64 * WR * WC), 0, s>>>(a, tiles_n);
   return hipGetLastError();

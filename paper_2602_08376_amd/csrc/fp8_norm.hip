@@ -133,7 +133,7 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(Norm8Args a) {
 }
 
 template <int XT, int RT>
-hipError_t launch(const Norm8Args& a, hipStream_t s) {
+hipError_t launch_slice(const Norm8Args& a, hipStream_t s) {
   const dim3 grid((unsigned)a.T);
 #define OJBKQ_NORM(NT, NV) rmsnorm_kernel<XT, RT, NT, NV><<<grid, dim3(NT), 0, s>>>(a)
   // few tokens leave CUs idle: many threads to each, for latency; otherwise
@@ -146,6 +146,26 @@ hipError_t launch(const Norm8Args& a, hipStream_t s) {
   else OJBKQ_NORM(1024, 0);
 #undef OJBKQ_NORM
   return hipGetLastError();
+}
+
+// A grid holds 2^32 - 1 threads along a dimension.
+template <int XT, int RT>
+hipError_t launch(const Norm8Args& a, hipStream_t s) {
+  const int64_t step = (int64_t)1 << 21;
+  for (int64_t t = 0; t < a.T; t += step) {
+    Norm8Args b = a;
+    b.T = a.T - t < step ? a.T - t : step;
+    b.x = static_cast<const typename Number<XT>::type*>(a.x) + t * a.ldx;
+    if (a.r_in) {
+      typedef typename Number<RT < 0 ? 0 : RT>::type R;
+      b.r_in = static_cast<const R*>(a.r_in) + t * a.ldr;
+      b.r_out = static_cast<R*>(a.r_out) + t * a.ldr;
+    }
+    b.X8 = a.X8 + t * a.ld8;
+    b.scales = a.scales + t * a.lds;
+    if (hipError_t e = launch_slice<XT, RT>(b, s); e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <int XT>
