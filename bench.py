@@ -92,12 +92,18 @@ def parse():
                     help="instead of the benchmark line: quantize a synthetic stack of layers in "
                          "order, each on the activations of the layers already quantized (formed "
                          "with the packed-code product), and report per-layer output errors")
+    ap.add_argument("--act8", action="store_true",
+                    help="with --mlp-stack: activations in 8 bits, quantized once a layer and "
+                         "multiplied with its codes in that form")
     ap.add_argument("--adaptive", action="store_true",
                     help="with --mlp-stack: pick lambda, alpha and K per layer on held-out tokens")
     ap.add_argument("--stack-layers", type=int, default=4)
     ap.add_argument("--stack-dim", type=int, default=4096)
     ap.add_argument("--stack-tokens", type=int, default=32768)
-    return ap.parse_args()
+    args = ap.parse_args()
+    if args.act8 and (args.adaptive or not args.mlp_stack):
+        ap.error("--act8 goes with --mlp-stack (without --adaptive)")
+    return args
 
 
 def sweep_k(args):
@@ -274,6 +280,11 @@ def mlp_stack(args):
     own quantized input), alpha = 0.6 is the paper's setting; and the
     dequantize-and-multiply kernel against the fp16 MFMA roofline.
 
+    With --act8 the quantized stack's activations are brought to 8 bits in
+    front of each layer and its codes multiplied with those (results in
+    bfloat16); the line then has that product's output error beside the one of
+    16-bit activations on the same inputs, and both calls' times.
+
     The full-precision forward pass and the SiLU between layers are the
     synthetic model, computed with torch; every quantization step and the
     quantized product run in the library."""
@@ -308,6 +319,7 @@ def mlp_stack(args):
     for mu, K in ((1.0, 0), (1.0, 16), (0.6, 0), (0.6, 16)):
         X, Xq = X0, X0
         errs, qtimes, dq, dq_tiles = [], [], [], []
+        errs8, dq8, quant8 = [], [], []
         for l, W in enumerate(Ws):
             torch.cuda.synchronize()
             t0 = time.perf_counter()
@@ -332,6 +344,19 @@ def mlp_stack(args):
             dq_tiles.append(ms_tiles)
             Y = W @ X                                  # the full-precision stack
             errs.append(float((Yq - Y).norm() / Y.norm()))
+            if args.act8:
+                Xp = Xq if pp is None else Xq.index_select(0, pp.long())
+                (X8, xs), ms = product_ms(lambda: ok.quantize_fp8(Xp, features_first=True))
+                quant8.append(ms)
+                need8 = ok.library().ojbkq_dequant_matmul_fp8_workspace_bytes(d, d, T)
+                ws8 = torch.empty(need8, dtype=torch.uint8, device=dev)
+                Y8, ms = product_ms(lambda: ok.dequant_matmul_fp8(P, q.scales, q.zeros, d, bits,
+                                                                  group, X8, xs, workspace=ws8,
+                                                                  dtype=torch.bfloat16))
+                dq8.append(ms)
+                Yq = Y8.float()
+                errs8.append(float((Yq - Y).norm() / Y.norm()))
+                del Xp, X8, xs, ws8, Y8
             X, Xq = silu(Y), silu(Yq)
             del Y, Yq, P, Xq16
         flops = 2.0 * d * d * T
@@ -346,6 +371,10 @@ def mlp_stack(args):
                                             "peak": PEAK_F16_MFMA_TFLOPS,
                                             "frac": flops / (min(dq) * 1e-3) / 1e12 /
                                             PEAK_F16_MFMA_TFLOPS}}
+        if args.act8:
+            line.update(relative_output_error_act8=errs8, quantize_fp8_ms=quant8,
+                        dequant_matmul_fp8_ms=dq8,
+                        dequant_matmul_fp8_tflops=flops / (min(dq8) * 1e-3) / 1e12)
         print(json.dumps(line), flush=True)
         log(f"stack alpha={mu} K={K}: errors {[round(e, 5) for e in errs]}")
 
