@@ -299,6 +299,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void product8_kernel(Product8Args 
       if ((st & 3) == 0 && st + 4 < nst) load_scales(st / 4 + 1);
       if ((st & 3) == 1 && (st | 3) + 1 < nst) part_scales(st / 4 + 1);
       if (st + BUFS - 1 < nst) load(st + BUFS - 1);
+      __builtin_amdgcn_s_setprio(0);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int x = 0; x < NX; ++x) {
@@ -308,6 +309,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void product8_kernel(Product8Args 
           read_x(st, x + 1);
         } else {
           // (behind the last stage these read what stands there, unused)
+          __builtin_amdgcn_s_setprio(1);
           if (st + 1 < nst) arrived(st + 1);
           read_w(st + 1, 0);
           read_x(st + 1, 0);
@@ -374,6 +376,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void product8_kernel(Product8Args 
       if ((st & 3) == 0 && st + 4 < nst) load_scales(st / 4 + 1);
       if ((st & 3) == 1 && (st | 3) + 1 < nst) part_scales(st / 4 + 1);
       if (st + BUFS - 1 < nst) load(st + BUFS - 1);
+      __builtin_amdgcn_s_setprio(0);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int x = 0; x < NX; ++x) {
@@ -383,6 +386,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void product8_kernel(Product8Args 
           read_x(st, x + 1);
         } else {
           // (behind the last stage these read what stands there, unused)
+          __builtin_amdgcn_s_setprio(1);
           if (st + 1 < nst) arrived(st + 1);
           read_x(st + 1, 0);
         }
