@@ -469,12 +469,25 @@ hipError_t launch_tiles(const Product8Args& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// A CU holds one workgroup of the larger tiles or two of 128 x 128, so the chip
+// takes them in rounds of 256 or 512 tiles.
+// kExact: 256 x 128 while their rounds are full to 15/16 (us for 256 x 128 / 128
+// x 128 at m = 4096, 4096 channels: 2048 tokens, one round, 70.9 / 73.0, 4096
+// 136.7 / 140.0, 8192 270 / 279; 1024, half a round, 62.7 / 49.4; 5000, 2.5
+// rounds, 189 / 177; 14336 channels, 600 tokens, 1.3 rounds, 122 / 106, 2048, 3.5
+// rounds, 257 / 250).
+// 16-bit results: a round of 256 x 256 does twice the work of one of 128 x 128
+// in 1.6 times the time (256 x 256 / 128 x 128: 4096 channels, 2048 tokens, half
+// a round, 61 / 49; 4096 74 / 95; 5000, 1.25 rounds, 125 / 118; 8192 142 / 174;
+// 14336 channels, 600 tokens 61 / 73, 2048 134 / 162; the rule misses up to 8%
+// where a last round is half full: 6144 125 / 137).
 template <int HOW>
 hipError_t launch_how(const Product8Args& a, hipStream_t s) {
   auto tiles = [&](int64_t tt, int64_t tc) { return (a.n + tc - 1) / tc * ((a.T + tt - 1) / tt); };
   if constexpr (HOW == kExact) {
-    return tiles(256, 128) >= 192 ? launch_tiles<256, 128, 4, 2, 3, HOW>(a, s)
-                                  : launch_tiles<128, 128, 2, 2, 2, HOW>(a, s);
+    const int64_t big = tiles(256, 128);
+    return 16 * big >= 15 * ((big + 255) / 256 * 256) ? launch_tiles<256, 128, 4, 2, 3, HOW>(a, s)
+                                                      : launch_tiles<128, 128, 2, 2, 2, HOW>(a, s);
   } else {
     return 100 * ((tiles(256, 256) + 255) / 256) <= 62 * ((tiles(128, 128) + 511) / 512)
                ? launch_tiles<256, 256, 2, 4, 2, HOW>(a, s)

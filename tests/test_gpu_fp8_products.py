@@ -288,3 +288,33 @@ def test_oracles_weights_are_the_layers():
     q = oi.unpack_codes(P.cpu().numpy().view(np.uint32), 256, 4)
     want = np.repeat(S.cpu().numpy(), 128, 1) * (q - np.repeat(Z.cpu().numpy(), 128, 1))
     assert np.allclose(W, want, rtol=1e-6)
+
+
+@pytest.mark.parametrize("m", [1, 130, 384, 500, 640, 1300])
+@pytest.mark.parametrize("n,T", [(1925, 3845), (2048, 4096)])
+def test_whole_rounds_of_float32_results(n, T, m):
+    # enough tiles of 256 tokens x 128 channels for one each on 256 CUs, from
+    # one block of features to several
+    X8, xs, *X = eight_bits(T, m, T + m, 1, 1)
+    W8, ws, W, w = eight_bits(n, m, n + m, 128, 1, spread=1.0)
+    check(ok.matmul_fp8(W8, ws, X8, xs, tokens_first=m % 4 == 0), (W, w), X, m % 4 == 0)
+    f = ws.float() * (1 + torch.rand(ws.shape, device=DEV))
+    check(ok.matmul_fp8(W8, f, X8, xs), (w * o8.expand(f.double().cpu().numpy(), n, m, 128), w), X)
+    P, S, Z, W = codes(n, m, 3, 128, m)
+    check(ok.dequant_matmul_fp8(P, S, Z, m, 3, 128, X8, xs), W, X)
+
+
+@pytest.mark.parametrize("y", ["bf16", "f16"])
+@pytest.mark.parametrize("m", [1, 130, 384, 500, 1300])
+@pytest.mark.parametrize("n,T", [(3871, 3900), (4096, 4096)])
+def test_whole_rounds_of_16_bit_results(n, T, m, y):
+    # the same of tiles of 256 tokens x 256 channels
+    X8, xs, *X = eight_bits(T, m, T + m, 1, 1)
+    W8, ws, W, w = eight_bits(n, m, n + m, 128, 1, spread=1.0)
+    first = m % 4 == 0
+    check(ok.matmul_fp8(W8, ws, X8, xs, tokens_first=first, dtype=TYPES[y]), (W, w), X, first)
+    f = ws.float() * (1 + torch.rand(ws.shape, device=DEV))
+    check(ok.matmul_fp8(W8, f, X8, xs, tokens_first=not first, dtype=TYPES[y]),
+          (w * o8.expand(f.double().cpu().numpy(), n, m, 128), w), X, not first)
+    P, S, Z, W = codes(n, m, 4, 128, m)
+    check(ok.dequant_matmul_fp8(P, S, Z, m, 4, 128, X8, xs, tokens_first=first, dtype=TYPES[y]), W, X, first)
