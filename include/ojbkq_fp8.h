@@ -103,7 +103,8 @@ int ojbkq_rmsnorm_fp8(const void* x, int32_t xtype, int64_t T, int64_t m, int64_
  *   numbers: a magnitude below 2^-126 may count as 0, one from 2^128 on as
  *   infinite.
  *   A NaN in a token or a channel comes out in all it meets; so does an
- *   infinite scale.  n, T in [1, 2^24], m in [1, 2^20].                     */
+ *   infinite scale, and an e8m0 scale of code 255 makes all it meets infinite or
+ *   NaN.  n, T in [1, 2^24], m in [1, 2^20].                                */
 int ojbkq_matmul_fp8(const uint8_t* W8, int64_t ldw, const void* w_scales, int32_t w_scale_type,
                      int32_t w_block_rows, int64_t ldws, int64_t n, int64_t m, const uint8_t* X8,
                      int64_t ldx, const uint8_t* x_scales, int64_t ldxs, int64_t T, void* Y,

@@ -647,6 +647,8 @@ def rmsnorm_fp8(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float,
     T, m, ldx = _matrix(x, "x", FP8_TYPES)
     dev = x.device
     if gain is not None:
+        if not isinstance(gain, torch.Tensor):
+            raise TypeError("gain must be a torch.Tensor")
         if gain.dtype != torch.float32 or gain.shape != (m,) or gain.device != dev or not gain.is_contiguous():
             raise ValueError(f"gain must be float32 of shape ({m},), contiguous, on {dev}")
     rtype, ldr = 0, m
@@ -708,7 +710,7 @@ def matmul_fp8(W8: torch.Tensor, w_scales: torch.Tensor, X8: torch.Tensor, x_sca
     n, mw, ldw = _padded(W8, "W8", E4M3, 16, dev)
     if mw != m:
         raise ValueError(f"W8 has {mw} features and X8 {m}")
-    rows = w_scales.shape[0] if w_scales.dim() == 2 else -1
+    rows = w_scales.shape[0] if isinstance(w_scales, torch.Tensor) and w_scales.dim() == 2 else -1
     if rows not in (n, -(-n // FP8_BLOCK)):
         raise ValueError(f"w_scales must have a row for each row or for each 128 rows of W8 (got {rows})")
     e8m0 = w_scales.dtype == E8M0
@@ -743,7 +745,7 @@ def dequant_matmul_fp8(packed: torch.Tensor, scales: torch.Tensor, zeros: torch.
     if mx != m:
         raise ValueError(f"X8 has {mx} features, expected {m}")
     ldxs = _padded(x_scales, "x_scales", E8M0, 4, dev, (T, -(-m // FP8_BLOCK)))[2]
-    n = packed.shape[0]
+    n = packed.shape[0] if isinstance(packed, torch.Tensor) and packed.dim() else 0
     _need(packed, "packed", torch.int32, (n, packed_words(m, bits)), dev)
     group = 0 if group >= m else int(group)
     G = num_groups(m, group)

@@ -10,12 +10,12 @@ __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)"
 // Y for few tokens.  Bound by reading the weights (for the fewest tokens by
 // latency), so a workgroup takes few channels, 16 RB, for all features, and its
 // eight waves split the features: chunks of 128 go round the waves, which meet
-// at the end in LDS, where their sums are added in wave order.  A lane's operands are 32 features of channel l % 16 and of token l %
-// 16, both brought to 16 bits in registers, a quarter of them to each of the
-// chunk's four products of 16 x 16 x 32.  (The matrix cores' 8-bit products
-// keep about 13 bits beside the largest of eight neighbours; these keep
-// float32's.)  The activations are the A operand, so a lane's four sums belong
-// to one channel and take its scale.
+// at the end in LDS, where their sums are added in wave order.  A lane's
+// operands are 32 features of channel l % 16 and of token l % 16, both brought to
+// 16 bits in registers, a quarter of them to each of the chunk's four products of
+// 16 x 16 x 32.  (The matrix cores' 8-bit products keep about 13 bits beside the
+// largest of eight neighbours; these keep float32's.)  The activations are the A
+// operand, so a lane's four sums belong to one channel and take its scale.
 //   e4m3 weights: both in bf16, which holds a value times a power of two.
 //   Codes: both in fp16, without the scales.  A code q set into the low bits of
 //   fp16's 1024 is 1024 + q, from which a packed subtraction takes 1024 + z:
@@ -27,6 +27,11 @@ __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)"
 // channels and tokens; they were the bound).  So a wave's rows come straight to
 // LDS, neighbouring lanes along a row, into a ring of kDepth chunks of its own;
 // no barrier is needed until the end.
+//
+// 4096 x 4096, one token: e4m3 6.2 us, 4-bit codes 6.8, of which the latency of a
+// launch, of the first loads and of the sums' meeting is the larger part (its 16.8
+// or 8.4 MB would pass in 3.2 or 1.6); 24 tokens, codes of 14336 x 4096: 15.5 us,
+// bound by the vector instructions that bring both operands to 16 bits.
 template <int SRC, int RB, int NB>
 struct Few {
   static constexpr int kTok = 16 * NB, kChan = 16 * RB, kWaves = 8;
