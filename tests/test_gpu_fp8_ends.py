@@ -256,3 +256,51 @@ def test_a_token_whose_features_are_all_masked():
     assert not Y[:, 5].any() and not Y[:, 69].any() and not bool(Y.isnan().any())
     want, e = o8.quantize(x.double().cpu().numpy())
     assert np.array_equal(X8.double().cpu().numpy(), want)
+
+
+def test_arguments_that_the_binding_refuses():
+    X8, xs = whole(40, 256, 16)
+    W8, ws = whole(30, 256, 17)
+    P, S, Z = random_codes(30, 256, 4, 128, 18)
+    x, gain = torch.randn(40, 256, device=DEV), torch.ones(256, device=DEV)
+    mm = ok.matmul_fp8
+    dq = lambda *a, **k: ok.dequant_matmul_fp8(*a, X8, xs, **k)  # noqa: E731
+    bad = [lambda: mm(W8, [1.0], X8, xs), lambda: mm(W8, ws[0], X8, xs), lambda: mm(W8, ws[:7], X8, xs),
+           lambda: mm(W8, ws.double(), X8, xs), lambda: mm(W8, ws.cpu(), X8, xs), lambda: mm(W8, ws, X8, xs[:39]),
+           lambda: mm(W8[:, :128], ws[:, :1], X8, xs), lambda: mm(W8, ws, X8[:, 1:], xs), lambda: mm(W8.t(), ws, X8, xs),
+           lambda: mm(W8, ws, X8, xs, dtype=torch.float64), lambda: mm(W8, ws, X8, ws), lambda: mm(W8, ws, x, xs),
+           lambda: dq(P, S, Z, 255, 4, 128), lambda: dq(P, S, Z, 256, 3, 128), lambda: dq(P, S[:, :1], Z, 256, 4, 128),
+           lambda: dq(P, S, Z.double(), 256, 4, 128), lambda: dq(P.t(), S, Z, 256, 4, 128), lambda: dq(P[0], S, Z, 256, 4, 128),
+           lambda: ok.rmsnorm_fp8(x, gain[:255], 1e-5), lambda: ok.rmsnorm_fp8(x, gain.half(), 1e-5),
+           lambda: ok.rmsnorm_fp8(x, gain, 1e-5, residual=x[:39]), lambda: ok.rmsnorm_fp8(x, gain, 1e-5, residual_out=x),
+           lambda: ok.rmsnorm_fp8(x, gain, 1e-5, residual=x.double()),
+           lambda: ok.rmsnorm_fp8(x, gain, 1e-5, residual=x, residual_out=torch.empty(40, 300, device=DEV)[:, :256]),
+           lambda: ok.quantize_fp8(x, block_rows=64), lambda: ok.quantize_fp8(x[:, ::2]),
+           lambda: ok.quantize_fp8(x[:1].expand(40, 256))]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            print("call", i)
+            call()
+    for call in (lambda: dq([1], S, Z, 256, 4, 128), lambda: ok.rmsnorm_fp8(x, 1.0, 1e-5), lambda: ok.rmsnorm_fp8(None, gain, 1e-5)):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: ok.quantize_fp8(x, block_rows=128, features_first=True), lambda: ok.rmsnorm_fp8(x, gain, -1.0),
+                 lambda: ok.rmsnorm_fp8(x, gain, float("nan")), lambda: ok.quantize_fp8(x[:0]),
+                 lambda: dq(P, torch.ones(30, 4, device=DEV), torch.ones(30, 4, device=DEV), 256, 4, 64)):
+        with pytest.raises(ok.OjbkqError):
+            call()
+
+
+def test_a_scale_that_is_no_number():
+    # an e8m0 code 255 makes its token's or its channels' results infinite or NaN, no others
+    for n, T in ((40, 20), (2100, 1003), (4096, 4096)):
+        X8, xs = whole(T, 256, 19, most=3)
+        W8, ws = whole(n, 256, 20, most=3)
+        X8, W8 = (X8.float().abs() + 1).to(F8), (W8.float().abs() + 1).to(F8)
+        bits(xs)[3, 1] = 255
+        bits(ws)[5, 0] = 255
+        for y in (torch.float32, torch.bfloat16):
+            Y = ok.matmul_fp8(W8, ws, X8, xs, dtype=y)
+            bad = torch.zeros(n, T, dtype=torch.bool, device=DEV)
+            bad[5], bad[:, 3] = True, True
+            assert torch.equal(~Y.isfinite(), bad), (n, T, y)
