@@ -37,15 +37,16 @@ __device__ __forceinline__ float from_e8m0(uint32_t code) {
 // A weight scale as a power of two, which goes to the weights in bf16 or in the
 // matrix instruction (exactly), and the rest, with which a block's sums are
 // multiplied: these then lie in the result's own range, whatever the scales.
-// (0, infinities, NaN and numbers below float32's normal range are all rest.)
+// (The rest is 1 to 2; below it for 0 and numbers under float32's normal range,
+// whose power is the range's least; all of an infinity or a NaN.)
 struct SplitScale {
   float power, rest;
 };
 __device__ __forceinline__ SplitScale split_scale(float s) {
   const uint32_t b = __float_as_uint(s), e = b & 0x7f800000u;
-  const bool odd = e == 0u || e == 0x7f800000u;
-  return {__uint_as_float(odd ? 0x3f800000u : e),
-          odd ? s : __uint_as_float((b & 0x807fffffu) | 0x3f800000u)};
+  if (e == 0u) return {0x1p-126f, s * 0x1p126f};
+  if (e == 0x7f800000u) return {1.f, s};
+  return {__uint_as_float(e), __uint_as_float((b & 0x807fffffu) | 0x3f800000u)};
 }
 
 // Eight e4m3 values times a power of two, exactly, in bf16 (whose 8 mantissa

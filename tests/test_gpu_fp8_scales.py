@@ -97,3 +97,67 @@ def test_a_code_of_255_among_codes(n, T):
         assert not bool(got[:, t].isfinite().any())
         keep = torch.arange(T, device=DEV) != t
         assert torch.equal(got[:, keep], want[:, keep])
+
+
+def large_weights(n, m, seed):
+    """e4m3 numbers of at least 16 in magnitude."""
+    rng = np.random.default_rng(seed)
+    w = o8.round_e4m3(np.exp2(rng.uniform(4, 8.8, (n, m))) * rng.choice([-1.0, 1.0], (n, m)))
+    return torch.from_numpy(w).float().to(F8).to(DEV), w
+
+
+def e8m0(codes, m):
+    """Scales of one row for each of `codes`' rows, padded to four."""
+    s = torch.zeros(codes.shape[0], -(-codes.shape[1] // 4) * 4, dtype=torch.uint8, device=DEV)
+    s[:, :codes.shape[1]] = codes
+    return s.view(E8)[:, :codes.shape[1]]
+
+
+PRODUCTS = [(40, 1), (300, 24), (6000, 24), (2100, 1003), (4096, 4096)]
+
+
+@pytest.mark.parametrize("y", ["f32", "bf16"])
+@pytest.mark.parametrize("n,T", PRODUCTS)
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -130, 1.7 * 2.0 ** -129, 2.0 ** -127, "e8m0"])
+def test_weight_scales_below_the_normal_range(scale, n, T, y):
+    # with activations near the largest float32: a block of weights 0, or of
+    # weights from 2^-126 on by a scale below it
+    m = 256
+    W8, w = large_weights(n, m, n)
+    X8, xs, X, x = eight_bits(T, m, T)
+    xs.view(torch.uint8)[:, 0] = 246
+    xs.view(torch.uint8)[:, 1] = 127
+    if scale == "e8m0":
+        ws = e8m0(torch.tensor([[0, 127]], dtype=torch.uint8, device=DEV).expand(n, 2), m)
+    else:
+        ws = torch.tensor([[scale, 1.0]], device=DEV).expand(n, 2).contiguous()
+    Y = ok.matmul_fp8(W8, ws, X8, xs, dtype=TYPES[y])
+    assert bool(Y.isfinite().all())
+    if scale == 0.0:
+        none = X8.clone().view(torch.uint8)
+        none[:, :128] = 0
+        assert torch.equal(Y, ok.matmul_fp8(W8, ws, none.view(F8), xs, dtype=TYPES[y]))
+        return
+    W = w * np.repeat(ws.double().cpu().numpy(), 128, 1)
+    check(Y, (W, w), (np.ldexp(x, np.repeat([[119, 0]], 128, 1)), x))
+
+
+@pytest.mark.parametrize("y", ["f32", "bf16"])
+@pytest.mark.parametrize("n,T", PRODUCTS)
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -127])
+def test_code_scales_below_the_normal_range(scale, n, T, y):
+    m = 256
+    P, S, Z, (_, w) = codes(n, m, 4, 128, n)
+    X8, xs, X, x = eight_bits(T, m, T)
+    xs.view(torch.uint8)[:, 0] = 246
+    xs.view(torch.uint8)[:, 1] = 127
+    S[:, 0] = scale
+    call = lambda v: ok.dequant_matmul_fp8(P, S, Z, m, 4, 128, v, xs, dtype=TYPES[y])  # noqa: E731
+    Y = call(X8)
+    assert bool(Y.isfinite().all())
+    if scale == 0.0:
+        none = torch.zeros(T, m, device=DEV)
+        none[:, 128:] = X8[:, 128:].float()
+        assert torch.equal(Y, call(none.to(F8)))
+        return
+    check(Y, times((None, w), S), (np.ldexp(x, np.repeat([[119, 0]], 128, 1)), x))
