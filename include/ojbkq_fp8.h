@@ -70,8 +70,10 @@ int ojbkq_quantize_fp8(const void* X, int32_t xtype, int64_t rows, int64_t m, in
  *     residual_out = h rounded to rtype,
  *     y = h gain / sqrt(mean(h^2) + eps)   (the mean over the token's features),
  *   and y is brought to 8 bits as by ojbkq_quantize_fp8 with block_rows = 1.
- *   Norm and rounding to 8 bits are those of float64 (y is not rounded in
- *   between); a y beyond float32's range counts as infinite.  A token whose h
+ *   Norm and rounding to 8 bits are those of float64: h gain is exact there, it
+ *   is divided by the root once, and y is not rounded in between (one that lies
+ *   on a border of e4m3 goes to the even side); a y beyond float32's range counts
+ *   as infinite.  A token whose h
  *   holds a NaN or an infinity comes out as NaN, and so does one of zeros with
  *   eps = 0 (0 / 0).
  *   x [T, m] type xtype, row stride ldx; residual_in, residual_out [T, m] type

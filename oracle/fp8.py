@@ -84,14 +84,15 @@ def dequantize(v: np.ndarray, e: np.ndarray, block_rows: int = 1) -> np.ndarray:
 
 
 def rmsnorm(x, residual, gain, eps):
-    """(y, h): h = x + residual summed in float32, y in float64."""
+    """(y, h): h = x + residual summed in float32, y = (h gain) / root in float64
+    (h gain is exact there)."""
     h = np.asarray(x, dtype=np.float32)
     if residual is not None:
         h = (h + np.asarray(residual, dtype=np.float32)).astype(np.float32)
     d = h.astype(np.float64)
     with np.errstate(invalid="ignore", over="ignore"):
-        y = d / np.sqrt(np.mean(d * d, axis=1, keepdims=True) + eps)
-        return (y if gain is None else y * np.asarray(gain, dtype=np.float64)), h
+        hg = d if gain is None else d * np.asarray(gain, dtype=np.float64)
+        return hg / np.sqrt(np.mean(d * d, axis=1, keepdims=True) + eps), h
 
 
 def matmul(W: np.ndarray, X: np.ndarray) -> np.ndarray:

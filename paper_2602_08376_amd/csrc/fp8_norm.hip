@@ -5,7 +5,9 @@
 namespace ojbkq {
 namespace {
 
-struct None {};   // no residual
+struct Root {
+  double inv, rest;   // 1 / sqrt(mean + eps), to twice float64's bits
+};
 
 template <class E>
 __device__ __forceinline__ void widen(const Eight<E>& x, float (&h)[8]) {
@@ -72,7 +74,7 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(Norm8Args a) {
     }
     return s;
   };
-  auto finish = [&](int64_t k, const float (&h)[8], double inv) {
+  auto finish = [&](int64_t k, const float (&h)[8], Root root) {
     if constexpr (kRes) {
       Eight<R> o;
 #pragma unroll
@@ -91,8 +93,14 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(Norm8Args a) {
     uint32_t hi[8], most = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      // (inv is NaN for a token with one; past the last feature h is 0)
-      hi[e] = k + e < a.m ? sticky_high((double)h[e] * inv * (double)g[e]) : 0u;
+      // h gain is exact in float64, and the reciprocal's second part makes the
+      // product the quotient rounded once: a y that lies on a border of e4m3
+      // stays there.  (NaN for a token with one; past the last feature h is 0.)
+      float v = h[e];
+      asm volatile("" : "+v"(v));   // (or the squares' float64 forms are kept in registers)
+      const double hg = (double)v * (double)g[e];
+      const double y = __builtin_fma(hg, root.inv, hg * root.rest);
+      hi[e] = k + e < a.m ? sticky_high(y) : 0u;
       const uint32_t s = size_key64(hi[e]);
       most = most > s ? most : s;
     }
@@ -101,9 +109,10 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(Norm8Args a) {
     if ((tid & 15) == 0 && k < a.m) a.scales[row * a.lds + (k >> 7)] = (uint8_t)code;
   };
   // infinite sums (an infinity in h) give NaN for the whole token
-  auto inverse = [&](double s) {
-    return s < __builtin_huge_val() ? 1.0 / __builtin_sqrt(s / (double)a.m + a.eps)
-                                    : __builtin_nan("");
+  auto root_of = [&](double s) {
+    const double v = __builtin_sqrt(s / (double)a.m + a.eps);
+    const double inv = s < __builtin_huge_val() ? 1.0 / v : __builtin_nan("");
+    return Root{inv, __builtin_fma(-v, inv, 1.0) * inv};
   };
 
   if constexpr (NV > 0) {
@@ -113,9 +122,9 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(Norm8Args a) {
     double s = 0.0;
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) s += squares(h[i]);
-    const double inv = inverse(total(s));
+    const Root root = root_of(total(s));
 #pragma unroll
-    for (int i = 0; i < kRuns; ++i) finish(8 * ((int64_t)tid + NT * i), h[i], inv);
+    for (int i = 0; i < kRuns; ++i) finish(8 * ((int64_t)tid + NT * i), h[i], root);
   } else {
     // every thread reads the same features both times, so the residual may be
     // updated in place
@@ -126,10 +135,10 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(Norm8Args a) {
       read(k, h);
       s += squares(h);
     }
-    const double inv = inverse(total(s));
+    const Root root = root_of(total(s));
     for (int64_t k = 8 * tid; k < whole; k += 8 * NT) {
       read(k, h);
-      finish(k, h, inv);
+      finish(k, h, root);
     }
   }
 }
