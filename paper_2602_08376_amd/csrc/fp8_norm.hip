@@ -30,7 +30,7 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(Norm8Args a) {
   typedef typename Number<RT < 0 ? 0 : RT>::type R;
   constexpr bool kRes = RT >= 0;
   constexpr int kRuns = NV ? NV : 1, kWaves = NT / 64;
-  __shared__ double part[kWaves];
+  __shared__ double part[kRuns * kWaves];
   const int tid = threadIdx.x;
   const int64_t row = blockIdx.x;
   const X* const x = static_cast<const X*>(a.x) + row * a.ldx;
@@ -61,18 +61,25 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(Norm8Args a) {
     for (int e = 0; e < 8; ++e) s = __builtin_fma((double)h[e], (double)h[e], s);
     return s;
   };
-  // the token's sum, in every thread
-  auto total = [&](double s) {
+  // The token's sum, in every thread: runs of 512 features by themselves (a
+  // wave's), then these in a fixed order, so that it does not go by how many
+  // threads and registers share the features.
+  auto total = [&](double (&s)[kRuns]) {
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d);
-    if constexpr (kWaves > 1) {
-      if ((tid & 63) == 0) part[tid >> 6] = s;
-      __syncthreads();
-      s = 0.0;
+    for (int d = 1; d < 64; d *= 2)
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) s += part[w];
-    }
-    return s;
+      for (int i = 0; i < kRuns; ++i) s[i] += __shfl_xor(s[i], d);
+    if ((tid & 63) == 0)
+#pragma unroll
+      for (int i = 0; i < kRuns; ++i) part[kWaves * i + (tid >> 6)] = s[i];
+    __syncthreads();
+    constexpr int kParts = kRuns * kWaves, kLanes = kParts <= 4 ? 4 : kParts <= 8 ? 8 : kParts <= 16 ? 16 : 32;
+    static_assert(kParts <= 32, "a lane to each");
+    const int lane = tid & (kLanes - 1);
+    double all = lane < kParts ? part[lane] : 0.0;
+#pragma unroll
+    for (int d = 1; d < kLanes; d *= 2) all += __shfl_xor(all, d);
+    return all;
   };
   auto finish = [&](int64_t k, const float (&h)[8], Root root) {
     if constexpr (kRes) {
@@ -119,21 +126,21 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(Norm8Args a) {
     float h[kRuns][8];
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) read(8 * ((int64_t)tid + NT * i), h[i]);
-    double s = 0.0;
+    double s[kRuns];
 #pragma unroll
-    for (int i = 0; i < kRuns; ++i) s += squares(h[i]);
+    for (int i = 0; i < kRuns; ++i) s[i] = squares(h[i]);
     const Root root = root_of(total(s));
 #pragma unroll
     for (int i = 0; i < kRuns; ++i) finish(8 * ((int64_t)tid + NT * i), h[i], root);
   } else {
     // every thread reads the same features both times, so the residual may be
     // updated in place
-    double s = 0.0;
+    double s[1] = {0.0};
     float h[8];
     const int64_t whole = (a.m + 127) / 128 * 128;   // whole rows of 16 lanes for max16
     for (int64_t k = 8 * tid; k < a.m; k += 8 * NT) {
       read(k, h);
-      s += squares(h);
+      s[0] += squares(h);
     }
     const Root root = root_of(total(s));
     for (int64_t k = 8 * tid; k < whole; k += 8 * NT) {

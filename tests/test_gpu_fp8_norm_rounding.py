@@ -70,3 +70,23 @@ def test_largest_magnitudes_on_the_scales_border():
     v, s = ok.rmsnorm_fp8(h[:, None].expand(6, 256).contiguous(), gain, 0.0)
     assert (exponents(s) == [[-8, 0]]).all()
     assert (host(v) == [256.0] * 128 + [448.0] * 128).all()
+
+
+@pytest.mark.parametrize("m", [4096, 8192])
+def test_a_token_by_itself_and_among_many(m):
+    # One square of 2^56 beside several of 8, of which float64 loses each that is
+    # added to it by itself and keeps those that are added up before: the root is
+    # 2^28 / sqrt(m) or two steps above, and a y of the second half on the border
+    # of e4m3 or below it.  The order of the sum does not go by the number of
+    # tokens, which chooses the threads to a token.
+    h = np.zeros(m, dtype=np.float32)
+    h[0] = 2.0 ** 28
+    for run in [0, 1, 2, 4, 8, 16, 32] + list(range(64, m // 16, 64)):
+        h[m // 2 + 8 * run:m // 2 + 8 * run + 2] = 2.0
+    gain = torch.ones(m, device=DEV)
+    gain[m // 2], gain[m // 2 + 1] = 19 / 16, 7 / 4
+    x = torch.from_numpy(h).to(DEV)
+    one = ok.rmsnorm_fp8(x[None], gain, 0.0)
+    for T in (2, 512, 513, 2000):
+        v, s = ok.rmsnorm_fp8(x.expand(T, m).contiguous(), gain, 0.0)
+        same(v, s, np.repeat(host(one[0]), T, 0), np.repeat(exponents(one[1]), T, 0))
