@@ -98,7 +98,6 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(Norm8Args a) {
       for (int e = 0; e < 8; ++e) g[e] = 1.f;
     }
     uint32_t hi[8], most = 0;
-    const int left = (int)(a.m - k);   // (compared in 32 bits, eight times)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       // h gain is exact in float64, and the reciprocal's second part makes the
@@ -108,7 +107,7 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(Norm8Args a) {
       asm volatile("" : "+v"(v));   // (or the squares' float64 forms are kept in registers)
       const double hg = (double)v * (double)g[e];
       const double y = __builtin_fma(hg, root.inv, hg * root.rest);
-      hi[e] = e < left ? sticky_high(y) : 0u;
+      hi[e] = k + e < a.m ? sticky_high(y) : 0u;
       const uint32_t s = size_key64(hi[e]);
       most = most > s ? most : s;
     }
