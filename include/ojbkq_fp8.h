@@ -73,13 +73,14 @@ int ojbkq_quantize_fp8(const void* X, int32_t xtype, int64_t rows, int64_t m, in
  *   Norm and rounding to 8 bits are those of float64: h gain is exact there, it
  *   is divided by the root once, and y is not rounded in between (one that lies
  *   on a border of e4m3 goes to the even side); a y beyond float32's range counts
- *   as infinite.  A token whose h
- *   holds a NaN or an infinity comes out as NaN, and so does one of zeros with
- *   eps = 0 (0 / 0).
+ *   as infinite.  A token whose h holds a NaN or an infinity comes out as NaN,
+ *   and so does one of zeros with eps = 0 (0 / 0).  A token's results do not go
+ *   by the other tokens or by how many they are.
  *   x [T, m] type xtype, row stride ldx; residual_in, residual_out [T, m] type
- *   rtype, row stride ldr (elements), both or neither given; they may be the
- *   same array (an update in place) and otherwise must not overlap, nor may
- *   residual_out overlap x.  gain [m] float32 (NULL: 1).  eps >= 0, finite.
+ *   rtype, row stride ldr (elements), both or neither given.  residual_out may be
+ *   residual_in (an update in place), or x where their rows and the size of their
+ *   elements agree, and must not overlap either otherwise.  gain [m] float32
+ *   (NULL: 1).  eps >= 0, finite.
  *   X8, scales as above.  T >= 1, 1 <= m <= 2^20, T <= 2^24.                */
 int ojbkq_rmsnorm_fp8(const void* x, int32_t xtype, int64_t T, int64_t m, int64_t ldx,
                       const void* residual_in, void* residual_out, int32_t rtype, int64_t ldr,

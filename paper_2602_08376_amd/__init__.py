@@ -609,6 +609,25 @@ def _fp8_empty(rows, m, block_rows, dev):
     return v if m % FP8_BLOCK == 0 else v[:, :m], s if G % 4 == 0 else s[:, :G]
 
 
+def _overlap(p, lp, q, lq, n, m, sizes):
+    """Whether two matrices [n, m] of elements of ``sizes`` bytes, at p and q with row strides lp and
+    lq (bytes, at least a row's), share a byte, other than as one array (same place, stride and size:
+    there a kernel reads each element before it writes it)."""
+    wp, wq = m * sizes[0], m * sizes[1]
+    if p + (n - 1) * lp + wp <= q or q + (n - 1) * lq + wq <= p:
+        return False
+    if lp == lq:
+        if p == q and wp == wq:
+            return False
+        # row i + d of the first is the last one that starts at or before row i of the second, by r bytes
+        d, r = divmod(q - p, lp)
+        return (r < wp and -n < d < n) or (r + wq > lp and -n < d + 1 < n)
+    # the last row of the second that starts before a row of the first ends
+    at = p + lp * torch.arange(n)
+    j = torch.div(at + (wp - 1 - q), lq, rounding_mode="floor").clamp_(max=n - 1)
+    return bool(((j >= 0) & (q + lq * j + wq > at)).any())
+
+
 def quantize_fp8(X: torch.Tensor, block_rows: int = 1, features_first: bool = False):
     """``ojbkq_quantize_fp8``: X brought to 8 bits, (values, scales) with values
     [rows, m] float8_e4m3fn and scales [ceil(rows / block_rows), ceil(m / 128)]
@@ -643,7 +662,7 @@ def rmsnorm_fp8(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float,
     x [T, m] float32, float16 or bfloat16; gain [m] float32 or None; residual
     [T, m] of any of these types or None.  The residual stream becomes h,
     rounded to its type: in place, or in ``residual_out`` (the residual's type
-    and strides)."""
+    and strides), which may be ``x`` itself but overlap neither otherwise."""
     T, m, ldx = _matrix(x, "x", FP8_TYPES)
     dev = x.device
     if gain is not None:
@@ -655,10 +674,18 @@ def rmsnorm_fp8(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float,
     if residual is not None:
         _, _, ldr = _matrix(residual, "residual", FP8_TYPES, (T, m), dev)
         rtype = FP8_TYPES[residual.dtype]
+        out = residual.data_ptr()
+        rsize, xsize = 4 if rtype == 0 else 2, 4 if x.dtype is torch.float32 else 2
         if residual_out is None:
             residual_out = residual
         elif _matrix(residual_out, "residual_out", (residual.dtype,), (T, m), dev)[2] != ldr:
             raise ValueError("residual_out must have the strides of residual")
+        elif _overlap(out, ldr * rsize, residual_out.data_ptr(), ldr * rsize, T, m, (rsize, rsize)):
+            raise ValueError("residual_out must not overlap residual")
+        else:
+            out = residual_out.data_ptr()
+        if _overlap(x.data_ptr(), ldx * xsize, out, ldr * rsize, T, m, (xsize, rsize)):
+            raise ValueError("x must not overlap the stream that is written")
     elif residual_out is not None:
         raise ValueError("residual_out needs a residual")
     with _device(dev):
