@@ -19,11 +19,11 @@ __device__ __forceinline__ void widen(const Eight<E>& x, float (&h)[8]) {
 // neighbouring features of h in registers (NT * 8 * NV >= m), so x and the
 // residual are read once: bound by memory.  The squares are summed in float64
 // (no finite h overflows), and y is formed and rounded from float64, which
-// costs no more than float32 here: the vector ALU does 64-bit products at the
-// rate of 32-bit ones, and memory leaves it about 70 operations an element.
+// memory leaves time for where there is a residual.
 // NV = 0: longer rows, read twice.
-// 8192 x 8192, bfloat16, with a residual: 95 to 103 us, 4.9 to 4.6 TB/s (a large
-// copy: 5.2); 1 x 4096: 3.4 us, latency.
+// 8192 x 8192, bfloat16, with a residual: 91 to 95 us, 5.1 to 4.9 TB/s (a large
+// copy: 5.2); float16 without one 63 to 67 us, 3.2 to 3.0 TB/s, bound by the
+// vector ALU and the wait for the token's sum; 1 x 4096: 3.3 us, latency.
 template <int XT, int RT, int NT, int NV>
 __global__ __launch_bounds__(NT) void rmsnorm_kernel(Norm8Args a) {
   typedef typename Number<XT>::type X;
@@ -157,22 +157,31 @@ hipError_t launch_slice(const Norm8Args& a, hipStream_t s) {
   // Few tokens leave CUs idle: more threads to each, for latency; otherwise
   // fewer threads with several loads each under way, as long as their
   // registers leave a CU two workgroups.  us, bfloat16 x and residual:
-  //   1 x 4096       (512, 1) 3.4   (256, 2) 3.9   (1024, 1) 4.2
-  //   512 x 4096     (512, 1) 5.9   (256, 2) 5.9
-  //   8192 x 4096    (512, 1) 55.4  (256, 2) 51.0
-  //   1 x 8192       (1024, 1) 4.5  (256, 4) 5.6
-  //   512 x 8192     (1024, 1) 10.2 (256, 4) 10.7
-  //   8192 x 8192    (1024, 1) 112  (256, 4) 101   (512, 2) 100, float32 84.7 against 87.2 (4096 x 8192)
-  //   5000 x 12000   (512, 3) 101   (1024, 4) 207, its registers in memory  (512, 0) 107
-  //   4096 x 16384   (1024, 2) 111  (512, 4) 122   (512, 0) 115
-  //   2048 x 32768   (1024, 0) 124  (1024, 4) 135
+  //   1 x 4096       (512, 1) 3.3   (256, 2) 3.8   (1024, 1) 4.2
+  //   512 x 4096     (512, 1) 5.9   (256, 2) 6.2
+  //   8192 x 4096    (512, 1) 55.4  (256, 2) 51.5
+  //   1 x 8192       (1024, 1) 4.5  (512, 2) 4.6   (256, 4) 5.8
+  //   512 x 8192     (1024, 1) 10.4 (512, 2) 10.5  (256, 4) 11.3
+  //   8192 x 8192    (1024, 1) 112  (512, 2) 97    (256, 4) 96, float32 81.9 against 85.1 (4096 x 8192)
+  //   5000 x 12000   (512, 3) 92.5  (1024, 2) 111  (512, 0) 107
+  //   4096 x 16384   (512, 4) 100   (1024, 2) 107  (512, 0) 115, (1024, 0) 120
+  //   2048 x 32768   (1024, 0) 121
+  // Without a residual less is read and fewer registers are held, so a workgroup's
+  // threads may be fewer still: 8192 x 8192 float16 (256, 4) 66, (512, 2) 73; 8192 x
+  // 6144 bfloat16 (256, 3) 49, (256, 4) 61, (512, 2) 63.
+  if constexpr (RT < 0)
+    if (a.T > 512 && a.m > 4096 && a.m <= 8192) {
+      if (a.m <= 6144) OJBKQ_NORM(256, 3);
+      else OJBKQ_NORM(256, 4);
+      return hipGetLastError();
+    }
   if (a.m <= 2048) OJBKQ_NORM(256, 1);
   else if (a.m <= 4096 && a.T <= 512) OJBKQ_NORM(512, 1);
   else if (a.m <= 4096) OJBKQ_NORM(256, 2);
   else if (a.m <= 8192 && a.T <= 512) OJBKQ_NORM(1024, 1);
   else if (a.m <= 8192) OJBKQ_NORM(512, 2);
   else if (a.m <= 12288) OJBKQ_NORM(512, 3);
-  else if (a.m <= 16384) OJBKQ_NORM(1024, 2);
+  else if (a.m <= 16384) OJBKQ_NORM(512, 4);
   else OJBKQ_NORM(1024, 0);
 #undef OJBKQ_NORM
   return hipGetLastError();

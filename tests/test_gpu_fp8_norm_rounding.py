@@ -31,7 +31,8 @@ def ties(m):
 
 
 @pytest.mark.parametrize("x", list(TYPES))
-@pytest.mark.parametrize("T,m", [(130, 256), (600, 130), (130, 5000), (40, 40000)])
+@pytest.mark.parametrize("T,m", [(130, 256), (600, 130), (130, 5000), (600, 5000), (600, 7000), (520, 9000), (520, 13000),
+                                 (40, 40000)])
 def test_rows_of_one_value(x, T, m):
     # h / sqrt(mean(h^2)) = 1 (the squares' sum and its root are exact), so y is
     # the gain; whole numbers h, most of which have no exact reciprocal
