@@ -670,30 +670,27 @@ def rmsnorm_fp8(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float,
             raise TypeError("gain must be a torch.Tensor")
         if gain.dtype != torch.float32 or gain.shape != (m,) or gain.device != dev or not gain.is_contiguous():
             raise ValueError(f"gain must be float32 of shape ({m},), contiguous, on {dev}")
-    rtype, ldr = 0, m
+    at, r_in, r_out, rtype, ldr = x.data_ptr(), None, None, 0, m
     if residual is not None:
         _, _, ldr = _matrix(residual, "residual", FP8_TYPES, (T, m), dev)
-        rtype = FP8_TYPES[residual.dtype]
-        out = residual.data_ptr()
-        rsize, xsize = 4 if rtype == 0 else 2, 4 if x.dtype is torch.float32 else 2
-        if residual_out is None:
-            residual_out = residual
-        elif _matrix(residual_out, "residual_out", (residual.dtype,), (T, m), dev)[2] != ldr:
-            raise ValueError("residual_out must have the strides of residual")
-        elif _overlap(out, ldr * rsize, residual_out.data_ptr(), ldr * rsize, T, m, (rsize, rsize)):
-            raise ValueError("residual_out must not overlap residual")
-        else:
-            out = residual_out.data_ptr()
-        if _overlap(x.data_ptr(), ldx * xsize, out, ldr * rsize, T, m, (xsize, rsize)):
+        rtype, r_in = FP8_TYPES[residual.dtype], residual.data_ptr()
+        xsize, rsize = 4 if x.dtype is torch.float32 else 2, 4 if rtype == 0 else 2
+        r_out = r_in
+        if residual_out is not None and residual_out is not residual:
+            if _matrix(residual_out, "residual_out", (residual.dtype,), (T, m), dev)[2] != ldr:
+                raise ValueError("residual_out must have the strides of residual")
+            r_out = residual_out.data_ptr()
+            if _overlap(r_in, ldr * rsize, r_out, ldr * rsize, T, m, (rsize, rsize)):
+                raise ValueError("residual_out must not overlap residual")
+        if _overlap(at, ldx * xsize, r_out, ldr * rsize, T, m, (xsize, rsize)):
             raise ValueError("x must not overlap the stream that is written")
     elif residual_out is not None:
         raise ValueError("residual_out needs a residual")
     with _device(dev):
         v, s = _fp8_empty(T, m, 1, dev)
-        _check(library().ojbkq_rmsnorm_fp8(_at(x), FP8_TYPES[x.dtype], T, m, ldx, _at(residual),
-                                           _at(residual_out), rtype, ldr, _at(gain), float(eps),
-                                           _at(v), _up(m, FP8_BLOCK), _at(s),
-                                           _up(s.shape[1], 4), _raw_stream(dev)))
+        _check(library().ojbkq_rmsnorm_fp8(at, FP8_TYPES[x.dtype], T, m, ldx, r_in, r_out, rtype,
+                                           ldr, _at(gain), float(eps), _at(v), _up(m, FP8_BLOCK),
+                                           _at(s), _up(s.shape[1], 4), _raw_stream(dev)))
     return v, s
 
 
