@@ -93,13 +93,3 @@ def rmsnorm(x, residual, gain, eps):
     with np.errstate(invalid="ignore", over="ignore"):
         hg = d if gain is None else d * np.asarray(gain, dtype=np.float64)
         return hg / np.sqrt(np.mean(d * d, axis=1, keepdims=True) + eps), h
-
-
-def matmul(W: np.ndarray, X: np.ndarray) -> np.ndarray:
-    """Y [n, T] of W [n, m] and X [T, m], both dequantized."""
-    return np.asarray(W, dtype=np.float64) @ np.asarray(X, dtype=np.float64).T
-
-
-def absolute(W: np.ndarray, X: np.ndarray) -> np.ndarray:
-    """The sums of the products' magnitudes, which error bounds go by."""
-    return np.abs(W) @ np.abs(X).T

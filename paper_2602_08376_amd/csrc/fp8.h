@@ -61,7 +61,7 @@ struct Product8Args {
   int64_t ldy;
   int ytype, tokens_first;
 };
-// One pass over the weights or codes for every 64 tokens (fp8_few.hip).
+// One pass over the weights or codes for every 16 or 32 tokens (fp8_few.hip).
 hipError_t launch_product_few8(const Product8Args& a, int bits, hipStream_t stream);
 // The product in the kernel that its sizes ask for (fp8_matmul.hip); bits = 0:
 // of W8, otherwise of packed codes, with product8_workspace_bytes(n, m, T)

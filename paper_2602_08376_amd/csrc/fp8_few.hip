@@ -18,9 +18,11 @@ __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)"
 // operand, so a lane's four sums belong to one channel and take its scale.
 //   e4m3 weights: both in bf16, which holds a value times a power of two.
 //   Codes: both in fp16, without the scales.  A code q set into the low bits of
-//   fp16's 1024 is 1024 + q, from which a packed subtraction takes 1024 + z:
-//   three operations to two codes, against six by way of float32 (14336 x 4096,
-//   24 tokens: 482 vector instructions a chunk of 32 channels and tokens).
+//   fp16's 1024 is 1024 + q, from which a packed subtraction takes 1024 + z: of
+//   two 4-bit codes a shift (but for the lowest ones), a mask, an or and the
+//   subtraction, against six operations by way of float32 (some 410 vector
+//   instructions beside the 32 products of a chunk of 64 channels and 32 tokens,
+//   240 of them for the codes).
 //
 // Read from memory that way, neighbouring lanes would be rows apart, and every
 // lane's 16 bytes an access of the cache by itself (690 accesses a chunk of 32
@@ -28,10 +30,12 @@ __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)"
 // LDS, neighbouring lanes along a row, into a ring of kDepth chunks of its own;
 // no barrier is needed until the end.
 //
-// 4096 x 4096, one token: e4m3 6.2 us, 4-bit codes 6.8, of which the latency of a
-// launch, of the first loads and of the sums' meeting is the larger part (its 16.8
-// or 8.4 MB would pass in 3.2 or 1.6); 24 tokens, codes of 14336 x 4096: 15.5 us,
-// bound by the vector instructions that bring both operands to 16 bits.
+// 4096 x 4096, one token, kernels in a graph: e4m3 6.0 us, 4-bit codes 6.6, of
+// which the latency of a launch, of the first loads and of the sums' meeting is the
+// larger part (its 16.8 or 8.4 MB would pass in 3.2 or 1.6); 24 tokens, codes of
+// 14336 x 4096: 16 us, bound by the vector instructions that bring both operands
+// to 16 bits.  Of 33 to 1000 tokens every 32 read and convert the weights anew:
+// 4096 x 4096, 256 tokens 28 us, some seven times the transfer.
 template <int SRC, int RB, int NB>
 struct Few {
   static constexpr int kTok = 16 * NB, kChan = 16 * RB, kWaves = 8;

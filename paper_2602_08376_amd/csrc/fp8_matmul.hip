@@ -95,7 +95,9 @@ __device__ __forceinline__ void store_run(E* p, const float (&v)[N], int64_t lef
 // of a stage stay in registers while its activations pass.  Both operands go
 // straight from memory to LDS in lines of 128 bytes, 16-byte chunk c of line l
 // at slot c ^ (l % 8), which spreads the operand reads of 16 lines x 4 chunks
-// over all banks.
+// over all banks (the conflicts that a profile counts, 0.2 to 0.3 for each LDS
+// instruction of kScaled and kExact, are some 8 cycles a stage and wave, and kPowers,
+// which does without the reads of the weight scales' rests, has none).
 // Line 16 x + i of the activations holds token 32 (x / 2) + 8 (i / 4) + 4 (x %
 // 2) + i % 4, line 16 y + i of a wave's 64 of weights channel 4 i + y: a lane
 // then ends up with runs of 8 tokens and of 4 channels, whichever is contiguous
@@ -110,12 +112,12 @@ __device__ __forceinline__ void store_run(E* p, const float (&v)[N], int64_t lef
 // a CU one workgroup, so 128 x 128, two to a CU, does better on few tiles.
 // Float32 results need bf16 operands in registers (twice the size) and so smaller
 // ones: a wave 64 x 64 in both, 256 x 128 with three stages in LDS.
-// 4096 x 4096 x 32768, float32 scales, bfloat16 results: 541 to 550 us, 2.0 PFLOP/s
-// (matrix cores busy 43% of the time, LDS 60%; beside each product stand four
-// FMAs that scale its sums); 4096 x 11008, 1999 tokens, e8m0: 87 us, 2.06; with
-// float32 results 165, 1.09 (bf16 products; 42%).  What is left is the waves
+// 4096 x 4096 x 32768, float32 scales, bfloat16 results: 543 to 585 us, 2.0 to 1.9
+// PFLOP/s (matrix cores busy 45% of the time; beside each product stand four
+// FMAs that scale its sums); 4096 x 11008, 1999 tokens, e8m0: 88 us, 2.05; with
+// float32 results 163, 1.10 (bf16 products; 43%).  What is left is the waves
 // waiting for each other at a stage's barrier, and power: zeros for operands are
-// 12% faster.  Three stages of 256 x 128 or 128 x 256 for 16-bit results: 98.9
+// 13% faster (502 us; at 1999 tokens 5%, 83 us).  Three stages of 256 x 128 or 128 x 256 for 16-bit results: 98.9
 // against 97.7 us and, where 256 x 256 serves, 667 against 538.
 enum { kPowers, kScaled, kExact };
 template <int TT, int TC, int WR, int WC, int BUFS, int HOW>
@@ -490,7 +492,7 @@ hipError_t launch_tiles(const Product8Args& a, hipStream_t s) {
 // rounds, 189 / 177; 14336 channels, 600 tokens, 1.3 rounds, 122 / 106, 2048, 3.5
 // rounds, 257 / 250).
 // 16-bit results: a round of 256 x 256 does twice the work of one of 128 x 128
-// in 1.6 times the time (256 x 256 / 128 x 128: 4096 channels, 2048 tokens, half
+// in 1.6 times the time (us for 256 x 256 / 128 x 128: 4096 channels, 2048 tokens, half
 // a round, 61 / 49; 4096 74 / 95; 5000, 1.25 rounds, 125 / 118; 8192 142 / 174;
 // 14336 channels, 600 tokens 61 / 73, 2048 134 / 162; the rule misses up to 8%
 // where a last round is half full: 6144 125 / 137).
@@ -508,13 +510,21 @@ hipError_t launch_how(const Product8Args& a, hipStream_t s) {
   }
 }
 
-// The kernel for few tokens takes up to 32 of them, and more while it launches
-// few workgroups (of 32 channels x 32 tokens at most): 27 us for 1000 of them at
-// m = 4096, where a round of 128-wide tiles takes 35 us however full, 48 us with
-// float32 results, and 14 or 20 us more expand the codes of 4096 and 14336
-// channels (both sides: 4096 channels, 256 tokens: 28.8 / 35.2 and codes 30.3 /
-// 49.9; 512 tokens: 53.9 / 35.9 and 56.8 / 49.4; float32 54.0 / 49.5, codes 56.0
-// / 61.9).  Both go with m.
+// The kernel for few tokens takes up to 32 of them, and more while blocks of 32
+// channels x 32 tokens are few (its workgroups take 16 to 64 channels of them):
+// 28 us for 1000 blocks at m = 4096, where a round of 128-wide tiles takes 35 us
+// however full, 48 us with float32 results, and 13 or 20 us more expand the codes
+// of 4096 and 14336 channels.  us for few tokens' kernel / tiles, 4096 channels:
+//                   e4m3, 16 bits   float32       codes, 16 bits  float32
+//   m = 1024,  256  12.5 / 11.8     12.9 / 15.9   13.8 / 18.5     14.2 / 21.8
+//              512  23.5 / 12.7     24.0 / 16.9   25.6 / 18.6     26.2 / 22.8
+//   m = 4096,  256  28.2 / 34.7     27.9 / 47.0   28.5 / 48.5     28.6 / 60.0
+//              512  52.8 / 35.5     53.1 / 47.9   55.0 / 47.9     55.4 / 60.0
+//   m = 14336, 256  65.4 / 108      64.4 / 150    73.2 / 132      73.4 / 171
+//              512  127 / 109       127 / 153     144 / 132       144 / 172
+// The limits are those of m = 4096.  Tiles' times grow faster with m, so near the
+// limits the slower kernel is taken elsewhere: up to 1.3 times the other's time at
+// m = 1024 (14336 channels, 128 tokens, float32, 21.9 / 16.7), 1.2 at 14336.
 bool few(int64_t n, int64_t T, bool codes, bool f32) {
   const int64_t most = codes ? (f32 ? 2304 : 1792) : (f32 ? 1792 : 1280);
   return T <= 32 || (n + 31) / 32 * ((T + 31) / 32) <= most;
