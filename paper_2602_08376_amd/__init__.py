@@ -623,7 +623,7 @@ def _overlap(p, lp, q, lq, n, m, sizes):
         d, r = divmod(q - p, lp)
         return (r < wp and -n < d < n) or (r + wq > lp and -n < d + 1 < n)
     # the last row of the second that starts before a row of the first ends
-    at = p + lp * torch.arange(n)
+    at = p + lp * torch.arange(n, device="cpu")
     j = torch.div(at + (wp - 1 - q), lq, rounding_mode="floor").clamp_(max=n - 1)
     return bool(((j >= 0) & (q + lq * j + wq > at)).any())
 
