@@ -349,7 +349,10 @@ hipError_t launch_rb(const Product8Args& a, hipStream_t s) {
   // round of workgroups, each of which reads the activations again (us for 64 /
   // 32 / 16 channels: codes 14336 x 4096, 24 tokens 16.5 / 19.1 / 27.4, 11008 x
   // 4096 16.1 / 19.1 / 21.5; for 32 / 16: codes 4096 x 11008, 32 tokens, 128
-  // and 256 workgroups, 20.3 / 15.9).  64 e4m3 channels do not fit in LDS twice.
+  // and 256 workgroups, 20.3 / 15.9; e4m3, m = 4096, 24 tokens: 4096 channels, 128
+  // and 256 workgroups, 8.1 / 6.9, 5120, 160 and 320, 8.6 / 11.3, 14336 16.9 /
+  // 21.6; one token 6.4 / 5.9, 7.1 / 9.5, 14.3 / 18.1).  64 e4m3 channels do not
+  // fit in LDS twice.
   if constexpr (SRC != 0)
     if ((a.n + 63) / 64 * gy >= 160) {
       product_few8_kernel<SRC, 4, NB><<<grid(4), dim3(512), 0, s>>>(a);
